@@ -284,6 +284,127 @@ int ctcbeam_decode_noalloc(const float* logprobs, const int32_t* lengths, int B,
  * workspace holds no decode record (never passed to a decode). */
 int ctcbeam_query_status(const void* workspace, hipStream_t stream, uint32_t* bits);
 
+/*
+ * Operators on rows of scores, one row per frame: what makes the decoders'
+ * input of a model's logits, and what trains the model on a teacher's frames.
+ * The call only enqueues kernels on `stream` (no host synchronisation, no
+ * allocation); concurrent calls need distinct workspaces.  Outputs may not
+ * overlap inputs or each other, except where a call says so (returns 1).
+ */
+#define CTCBEAM_TYPE_F32 0
+#define CTCBEAM_TYPE_F16 1
+#define CTCBEAM_TYPE_BF16 2
+#define CTCBEAM_MAX_LABELS 262144 /* W, labels of a row */
+#define CTCBEAM_MAX_TOP 128       /* k, listed labels of a row */
+#define CTCBEAM_MAX_ROWS 8388608  /* B * T */
+
+/* Device scores [B, T, W] (for the decoders W = V+1, blank last).  The labels
+ * of a row are adjacent; utterances and frames lie stride_b and stride_t
+ * elements apart (>= 0; 0 repeats a row), so that [T, B, W] tensors and
+ * slices are taken as they are. */
+typedef struct ctcbeam_rows {
+  const void* data;
+  int type;               /* CTCBEAM_TYPE_* */
+  int B, T, W;
+  int64_t stride_b, stride_t;
+  const int32_t* lengths; /* device [B] or NULL (all T); clamped to [0, T];
+                             frames t >= L_b are not read */
+} ctcbeam_rows;
+
+typedef struct ctcbeam_process_opts {
+  const int32_t* history;         /* device [B, history_size] labels emitted before,
+                                     rows history_stride apart, or NULL; ids outside
+                                     0..W-1 (-1 as padding) are ignored */
+  int history_size;
+  int64_t history_stride;
+  const int32_t* history_lengths; /* device [B] or NULL (all); clamped */
+  const float* penalties;         /* device [B, 3] repetition, presence, frequency of
+                                     each utterance, or NULL: the three below */
+  float repetition, presence, frequency;
+  const float* bias;              /* device fp32 rows of W, bias_stride apart (0: one
+                                     for all utterances), or NULL */
+  int64_t bias_stride;
+  const uint32_t* mask;           /* device bit words of the allowed labels, label c in
+                                     bit c%32 of word c/32, ceil(W/32) words a row, rows
+                                     mask_stride_b / mask_stride_t words apart (0: the
+                                     same row); NULL: all are allowed */
+  int64_t mask_stride_b, mask_stride_t;
+  int normalize;                  /* 1: log-probabilities; 0: processed scores */
+  int reserved[3];
+} ctcbeam_process_opts;
+
+/*
+ * Penalties for repeated tokens, biases and grammar masks on logits; the
+ * result is what the decode calls take as log-probabilities.  Per label c,
+ * with n the occurrences of c in the utterance's history, in fp32:
+ *   x = logit (NaN: -inf; +inf: the largest finite number)
+ *   if n > 0: x = x > 0 ? x / repetition : x * repetition;
+ *             x = (x - frequency * n) - presence
+ *   x = x + bias[c] (NaN: -inf; +inf: the largest finite number)
+ *   a barred label: x = -inf
+ *   normalize: x = x - log(sum over the row of exp(x)); a row in which
+ *              nothing is allowed stays at -inf
+ *   out : device fp32 [B, T, W], contiguous; may be the logits themselves
+ *         where those are contiguous fp32.  Frames t >= L_b are left as they
+ *         were.
+ *   opts may be NULL (log-softmax).  workspace: of
+ *   ctcbeam_process_workspace_bytes(B, T, W) bytes (NULL where that is 0).
+ * Scalar penalties: repetition must be positive, all finite (else 1); those
+ * in device memory are taken as they are.
+ */
+size_t ctcbeam_process_workspace_bytes(int B, int T, int W);
+int ctcbeam_process_logits(const ctcbeam_rows* logits, const ctcbeam_process_opts* opts,
+                           float* out, void* workspace, size_t workspace_bytes,
+                           hipStream_t stream);
+
+/*
+ * The k largest logits of every row (descending; equal values: lowest label
+ * first; NaN counts as -inf and +inf as the largest finite number) and
+ *   tail = log(sum over the labels not listed of exp(logit / temperature)),
+ * -inf where nothing is left.  With the list this is the whole distribution's
+ * mass, without the cancellation of 1 - sum p.
+ *   k           : 1..min(W, CTCBEAM_MAX_TOP)
+ *   values, ids : device fp32 / int32 [B, T, k]; tail: device fp32 [B, T].
+ *   Frames t >= L_b get values -inf, ids -1 and tail -inf.
+ */
+size_t ctcbeam_top_workspace_bytes(int B, int T, int W, int k);
+int ctcbeam_top_logits(const ctcbeam_rows* logits, int k, float temperature, float* values,
+                       int32_t* ids, float* tail, void* workspace, size_t workspace_bytes,
+                       hipStream_t stream);
+
+/*
+ * Distillation from a teacher's top logits: per frame the divergence of the
+ * student's distribution from the teacher's, both at `temperature`, and its
+ * gradient.  With s = 1/temperature, u_i = s * top_values[i],
+ * Z = sum_i exp(u_i) + exp(tail):
+ *   P_c = sum of exp(u_i)/Z over the entries of label c; P_r = exp(tail)/Z
+ *   q = softmax(s * student row); q_r = sum of q over the labels not listed
+ *   loss = sum_c P_c (log P_c - log q_c) + P_r (log P_r - log q_r)
+ *   grad_c = weight * s * (q_c - P_c) for listed labels,
+ *            weight * s * (q_c - P_r * q_c / q_r) for the others.
+ * Without `tail` (NULL, or -inf) the list is renormalised.  Entries whose id
+ * lies outside 0..W-1 or whose value is -inf or NaN are no entries (their
+ * labels are not listed); +inf counts as the largest finite number.  A frame
+ * t >= L_b, a row without entries and tail, and a student row of -inf alone
+ * give loss 0 and gradient 0.  A listed label that the student bars (-inf)
+ * gives loss +inf and a finite gradient; NaN or +inf in a student row gives
+ * NaN.
+ *   top_values, top_ids : device [B, T, k], k in 1..CTCBEAM_MAX_TOP
+ *   tail    : device [B, T] or NULL, log-sum at `temperature`
+ *   weights : device, weight of row (b, t) at b*weight_stride_b +
+ *             t*weight_stride_t, or NULL: `weight`.  Only grad is weighted.
+ *   loss    : device fp32 [B, T], or NULL
+ *   grad    : device, of the student's type, rows grad_stride_b / _t elements
+ *             apart and not on each other, or NULL; one of the two is needed.
+ *             All frames are written.
+ */
+size_t ctcbeam_distill_workspace_bytes(int B, int T, int W);
+int ctcbeam_distill(const ctcbeam_rows* student, const float* top_values, const int32_t* top_ids,
+                    const float* tail, int k, float temperature, const float* weights,
+                    int64_t weight_stride_b, int64_t weight_stride_t, float weight, float* loss,
+                    void* grad, int64_t grad_stride_b, int64_t grad_stride_t, void* workspace,
+                    size_t workspace_bytes, hipStream_t stream);
+
 /* Thread-local message for the last non-zero return of this thread. */
 const char* ctcbeam_last_error(void);
 

@@ -30,6 +30,9 @@ _lib = None
 MAX_K = 128           # CTCBEAM_MAX_K (beams above 64 need V <= 1024)
 MAX_V = 4096
 MAX_ORDER = 8
+MAX_LABELS = 1 << 18  # CTCBEAM_MAX_LABELS
+MAX_TOP = 128         # CTCBEAM_MAX_TOP
+MAX_ROWS = 1 << 23    # CTCBEAM_MAX_ROWS
 
 
 class CtcbeamError(RuntimeError):
@@ -95,6 +98,19 @@ def _load():
     lib.ctcbeam_lm_tables.argtypes = [P, P]
     lib.ctcbeam_boost_tables.restype = I
     lib.ctcbeam_boost_tables.argtypes = [P, P]
+    S, L = ctypes.c_size_t, ctypes.c_int64
+    lib.ctcbeam_process_workspace_bytes.restype = S
+    lib.ctcbeam_process_workspace_bytes.argtypes = [I, I, I]
+    lib.ctcbeam_top_workspace_bytes.restype = S
+    lib.ctcbeam_top_workspace_bytes.argtypes = [I, I, I, I]
+    lib.ctcbeam_distill_workspace_bytes.restype = S
+    lib.ctcbeam_distill_workspace_bytes.argtypes = [I, I, I]
+    lib.ctcbeam_process_logits.restype = I
+    lib.ctcbeam_process_logits.argtypes = [P, P, P, P, S, P]
+    lib.ctcbeam_top_logits.restype = I
+    lib.ctcbeam_top_logits.argtypes = [P, I, F, P, P, P, P, S, P]
+    lib.ctcbeam_distill.restype = I
+    lib.ctcbeam_distill.argtypes = [P, P, P, P, I, F, P, L, L, F, P, P, L, L, P, S, P]
     _lib = lib
     return lib
 
@@ -512,3 +528,270 @@ def decode_nbest(logprobs, lengths, K: int, **kw):
     """Convenience: returns N-best (tokens [B,K,T], lengths [B,K], scores [B,K])."""
     tok, ln, sc, _ = ctcbeam_decode_nbest(logprobs, lengths, K, **kw)
     return tok, ln, sc
+
+
+# ------------------------------------------------ operators on rows of scores
+
+class _Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("type", ctypes.c_int), ("B", ctypes.c_int),
+                ("T", ctypes.c_int), ("W", ctypes.c_int), ("stride_b", ctypes.c_int64),
+                ("stride_t", ctypes.c_int64), ("lengths", ctypes.c_void_p)]
+
+
+class _ProcessOpts(ctypes.Structure):
+    _fields_ = [("history", ctypes.c_void_p), ("history_size", ctypes.c_int),
+                ("history_stride", ctypes.c_int64), ("history_lengths", ctypes.c_void_p),
+                ("penalties", ctypes.c_void_p), ("repetition", ctypes.c_float),
+                ("presence", ctypes.c_float), ("frequency", ctypes.c_float),
+                ("bias", ctypes.c_void_p), ("bias_stride", ctypes.c_int64),
+                ("mask", ctypes.c_void_p), ("mask_stride_b", ctypes.c_int64),
+                ("mask_stride_t", ctypes.c_int64), ("normalize", ctypes.c_int),
+                ("reserved", ctypes.c_int * 3)]
+
+
+_TYPES = {"torch.float32": 0, "torch.float16": 1, "torch.bfloat16": 2}   # CTCBEAM_TYPE_*
+
+
+def _need(t, dtype, name, dev):
+    import torch
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a device tensor")
+    if t.device != dev:
+        raise ValueError(f"{name} is on {t.device}, the inputs on {dev}")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+
+
+def _pointer(t, dtype, name, shape, dev):
+    """Address of a contiguous device tensor (None stays None)."""
+    if t is None:
+        return None
+    _need(t, dtype, name, dev)
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _rows_of(x, lengths, name):
+    """(ctcbeam_rows, B, T, W, device) of scores [B, T, W] with adjacent labels."""
+    import torch
+    _need(x, None, name, getattr(x, "device", None))
+    code = _TYPES.get(str(x.dtype))
+    if code is None:
+        raise TypeError(f"{name} must be float32, float16 or bfloat16, got {x.dtype}")
+    if x.dim() != 3:
+        raise ValueError(f"{name} must be [B, T, W]")
+    B, T, W = x.shape
+    sb, st, sl = x.stride()
+    if sl != 1 and W > 1:
+        raise ValueError(f"the labels of a row of {name} must be adjacent")
+    dev = x.device
+    return _Rows(x.data_ptr(), code, B, T, W, sb, st,
+                 _pointer(lengths, torch.int32, "lengths", (B,), dev)), B, T, W, dev
+
+
+def _workspace(workspace, need, dev, owned):
+    """(tensor or None, address, bytes): the given workspace, or one of ``need`` bytes."""
+    import torch
+    if workspace is None:
+        if not need:
+            return None, None, 0
+        workspace = torch.empty((need,), dtype=torch.uint8, device=dev)
+        owned.append(workspace)
+    return workspace, _dptr(workspace, torch.uint8, "workspace", None, dev), workspace.numel()
+
+
+def ctcbeam_process_logits(logits, lengths=None, history=None, history_lengths=None, penalties=None,
+                           repetition: float = 1.0, presence: float = 0.0, frequency: float = 0.0,
+                           bias=None, mask=None, normalize: bool = True, out=None, workspace=None,
+                           stream=None):
+    """Penalties for repeated tokens, biases and grammar masks on logits, on
+    ``stream``: what the decode calls take as ``logprobs``.
+
+    logits: float32, float16 or bfloat16 [B, T, W] with adjacent labels (any
+    utterance and frame strides); lengths: int32 [B].  history: int32 [B, H],
+    the tokens emitted before (ids outside 0..W-1 are ignored), of which the
+    first ``history_lengths`` [B] count; penalties: float32 [B, 3] (repetition,
+    presence, frequency of each utterance), else the three numbers.  bias:
+    float32 [W] or [B, W].  mask: int32 [ceil(W/32)], [B, ceil(W/32)] or
+    [B, T, ceil(W/32)], bit c%32 of word c/32 set where label c is allowed.
+    ``normalize=False`` leaves out the log-softmax.  Frames behind an
+    utterance's length are left as they were in ``out``, which may be the
+    logits themselves where those are contiguous float32.  No gradient flows
+    through this call.  Returns (float32 [B, T, W], workspace or None)."""
+    import torch
+    lib = _load()
+    rows, B, T, W, dev = _rows_of(logits, lengths, "logits")
+    owned = []
+    out = _alloc(out, (B, T, W), torch.float32, dev, owned)
+    o = _ProcessOpts(repetition=repetition, presence=presence, frequency=frequency, normalize=bool(normalize))
+    if history is not None:
+        _need(history, torch.int32, "history", dev)
+        if history.dim() != 2 or history.shape[0] != B:
+            raise ValueError(f"history must be [{B}, H], got {tuple(history.shape)}")
+        H = history.shape[1]
+        if H > 1 and history.stride(1) != 1:
+            raise ValueError("the tokens of a row of history must be adjacent")
+        if H:
+            o.history, o.history_size, o.history_stride = history.data_ptr(), H, history.stride(0)
+            o.history_lengths = _pointer(history_lengths, torch.int32, "history_lengths", (B,), dev)
+    elif history_lengths is not None:
+        raise ValueError("history_lengths without history")
+    if penalties is not None:
+        o.penalties = _pointer(penalties, torch.float32, "penalties", (B, 3), dev)
+    if bias is not None:
+        _need(bias, torch.float32, "bias", dev)
+        if bias.shape != (W,) and bias.shape != (B, W):
+            raise ValueError(f"bias must be [{W}] or [{B}, {W}], got {tuple(bias.shape)}")
+        if W > 1 and bias.stride(-1) != 1:
+            raise ValueError("the labels of a row of bias must be adjacent")
+        o.bias, o.bias_stride = bias.data_ptr(), 0 if bias.dim() == 1 else bias.stride(0)
+    if mask is not None:
+        _need(mask, torch.int32, "mask", dev)
+        words = (W + 31) // 32
+        if mask.shape != (words,) and mask.shape != (B, words) and mask.shape != (B, T, words):
+            raise ValueError(f"mask must be [{words}], [{B}, {words}] or [{B}, {T}, {words}], got {tuple(mask.shape)}")
+        if words > 1 and mask.stride(-1) != 1:
+            raise ValueError("the words of a row of mask must be adjacent")
+        o.mask = mask.data_ptr()
+        o.mask_stride_b = mask.stride(0) if mask.dim() > 1 else 0
+        o.mask_stride_t = mask.stride(1) if mask.dim() > 2 else 0
+    workspace, wp, wn = _workspace(workspace, lib.ctcbeam_process_workspace_bytes(B, T, W), dev, owned)
+    op = _pointer(out, torch.float32, "out", (B, T, W), dev)
+    _launch(lambda st: lib.ctcbeam_process_logits(ctypes.byref(rows), ctypes.byref(o), op, wp, wn, st),
+            dev, stream, owned)
+    return out, workspace
+
+
+def ctcbeam_top_logits(logits, k: int, lengths=None, temperature: float = 1.0, values=None, ids=None,
+                       tail=None, workspace=None, stream=None):
+    """The k largest logits of every row, on ``stream``: (values float32
+    [B, T, k] descending, ids int32 [B, T, k], tail float32 [B, T], workspace
+    or None), tail the log-sum of exp(logit / temperature) over the labels that
+    are not listed.  Equal values: the lowest label first; frames behind an
+    utterance's length get -inf, -1 and -inf.  No gradient flows through this
+    call."""
+    import torch
+    lib = _load()
+    rows, B, T, W, dev = _rows_of(logits, lengths, "logits")
+    k = int(k)
+    owned = []
+    kk = max(k, 0)
+    values = _alloc(values, (B, T, kk), torch.float32, dev, owned)
+    ids = _alloc(ids, (B, T, kk), torch.int32, dev, owned)
+    tail = _alloc(tail, (B, T), torch.float32, dev, owned)
+    workspace, wp, wn = _workspace(workspace, lib.ctcbeam_top_workspace_bytes(B, T, W, k), dev, owned)
+    vp = _pointer(values, torch.float32, "values", (B, T, kk), dev)
+    ip = _pointer(ids, torch.int32, "ids", (B, T, kk), dev)
+    tp = _pointer(tail, torch.float32, "tail", (B, T), dev)
+    _launch(lambda st: lib.ctcbeam_top_logits(ctypes.byref(rows), k, temperature, vp, ip, tp, wp, wn, st),
+            dev, stream, owned)
+    return values, ids, tail, workspace
+
+
+def ctcbeam_distill(student, values, ids, tail=None, lengths=None, temperature: float = 1.0, weights=1.0,
+                    want_loss: bool = True, want_grad: bool = True, loss=None, grad=None, workspace=None,
+                    stream=None):
+    """Distillation from a teacher's top logits, on ``stream``: the divergence
+    of every frame (float32 [B, T], unweighted) and, in the same pass over the
+    student's logits, ``weights`` (a number, or float32 [B, T] of any strides)
+    times its gradient, of the student's type.
+
+    student: float32, float16 or bfloat16 [B, T, W]; values, ids, tail: as
+    ``ctcbeam_top_logits`` gives them (``tail=None``: the list is renormalised).
+    ``grad`` may have any utterance and frame strides whose rows do not
+    overlap.  Returns (loss or None, grad or None, workspace or None)."""
+    import torch
+    lib = _load()
+    rows, B, T, W, dev = _rows_of(student, lengths, "student")
+    owned = []
+    _need(values, torch.float32, "values", dev)
+    if values.dim() != 3:
+        raise ValueError("values must be [B, T, k]")
+    k = values.shape[2]
+    vp = _pointer(values, torch.float32, "values", (B, T, k), dev)
+    ip = _pointer(ids, torch.int32, "ids", (B, T, k), dev)
+    tp = _pointer(tail, torch.float32, "tail", (B, T), dev)
+    if ip is None:
+        raise TypeError("ids must be a device tensor")
+    weight, w, wsb, wst = 1.0, None, 0, 0
+    if isinstance(weights, torch.Tensor):
+        _need(weights, torch.float32, "weights", dev)
+        if weights.shape != (B, T):
+            raise ValueError(f"weights must have shape {(B, T)}, got {tuple(weights.shape)}")
+        w, (wsb, wst) = weights.data_ptr(), weights.stride()
+    elif weights is not None:
+        weight = float(weights)
+    lp = gp = None
+    gsb = gst = 0
+    if want_loss or loss is not None:
+        loss = _alloc(loss, (B, T), torch.float32, dev, owned)
+        lp = _pointer(loss, torch.float32, "loss", (B, T), dev)
+    if want_grad or grad is not None:
+        grad = _alloc(grad, (B, T, W), student.dtype, dev, owned)
+        _need(grad, student.dtype, "grad", dev)
+        if grad.shape != (B, T, W):
+            raise ValueError(f"grad must have shape {(B, T, W)}, got {tuple(grad.shape)}")
+        gsb, gst, gsl = grad.stride()
+        if W > 1 and gsl != 1:
+            raise ValueError("the labels of a row of grad must be adjacent")
+        gp = grad.data_ptr()
+    workspace, wp, wn = _workspace(workspace, lib.ctcbeam_distill_workspace_bytes(B, T, W), dev, owned)
+    _launch(lambda st: lib.ctcbeam_distill(ctypes.byref(rows), vp, ip, tp, k, temperature, w, wsb, wst, weight,
+                                           lp, gp, gsb, gst, wp, wn, st), dev, stream, owned)
+    return loss, grad, workspace
+
+
+def process_logits(logits, lengths=None, **kw):
+    """Convenience: the processed scores alone."""
+    return ctcbeam_process_logits(logits, lengths, **kw)[0]
+
+
+def top_logits(logits, k: int, lengths=None, **kw):
+    """Convenience: returns (values, ids, tail)."""
+    return ctcbeam_top_logits(logits, k, lengths, **kw)[:3]
+
+
+def distill(student, values, ids, tail=None, lengths=None, **kw):
+    """Convenience: returns (loss or None, grad or None)."""
+    return ctcbeam_distill(student, values, ids, tail, lengths, **kw)[:2]
+
+
+_distill_function = None
+
+
+def distill_loss(student, values, ids, tail=None, lengths=None, temperature: float = 1.0):
+    """The divergence of every frame (float32 [B, T]) as a function that torch
+    differentiates with respect to ``student``; the teacher's list is a
+    constant.  Forward and backward read the student's logits once each
+    (``distill`` gives both in one pass where the frames' weights are known).
+    Not for capture into a graph while ``student`` needs a gradient: there
+    ``distill`` gives loss and gradient without torch's bookkeeping, whose
+    nodes belong to the stream they were made on."""
+    import torch
+    global _distill_function
+    if _distill_function is None:
+        class Distill(torch.autograd.Function):
+            @staticmethod
+            def forward(ctx, student, values, ids, tail, lengths, temperature):
+                ctx.save_for_backward(student, values, ids, tail, lengths)
+                ctx.temperature = temperature
+                return distill(student, values, ids, tail, lengths, temperature=temperature, want_grad=False)[0]
+
+            @staticmethod
+            @torch.autograd.function.once_differentiable
+            def backward(ctx, upstream):
+                student, values, ids, tail, lengths = ctx.saved_tensors
+                grad = distill(student, values, ids, tail, lengths, temperature=ctx.temperature,
+                               weights=upstream, want_loss=False)[1]
+                return grad, None, None, None, None, None
+        _distill_function = Distill
+    for name, t in (("values", values), ("tail", tail)):
+        if isinstance(t, torch.Tensor) and t.requires_grad:
+            raise ValueError(f"{name} is a constant of the loss: detach it")
+    if isinstance(student, torch.Tensor) and student.requires_grad and torch.is_grad_enabled() and \
+            student.is_cuda and torch.cuda.is_current_stream_capturing():
+        raise RuntimeError("distill_loss is not captured with a gradient: use distill, which gives loss and gradient")
+    return _distill_function.apply(student, values, ids, tail, lengths, float(temperature))

@@ -41,12 +41,13 @@ KERNEL_UNITS = ["ctcbeam_kernel_lpt1.hip", "ctcbeam_kernel_lpt2.hip", "ctcbeam_k
                 "ctcbeam_kernel_lpt4_rep.hip", "ctcbeam_kernel_lpt8_rep.hip", "ctcbeam_class_lpt1.hip", "ctcbeam_class_lpt2.hip",
                 "ctcbeam_class_lpt4.hip", "ctcbeam_class_lpt8.hip", "ctcbeam_greedy_v256.hip", "ctcbeam_greedy_v1024.hip",
                 "ctcbeam_greedy_v4096.hip", "ctcbeam_workspace.hip",
-                "ctcbeam_noalloc.hip", "ctcbeam_small.hip"]
+                "ctcbeam_noalloc.hip", "ctcbeam_small.hip", "ctcbeam_rows.hip"]
+HOST_UNITS = ["ctcbeam_host.cpp", "ctcbeam_rows_host.cpp"]
 
 
 def build(verbose: bool = False, jobs: int = 0, phase_clocks: bool = False) -> str:
     from concurrent.futures import ThreadPoolExecutor
-    jobs = jobs or max(1, min(len(KERNEL_UNITS) + 1, os.cpu_count() or 1))
+    jobs = jobs or max(1, min(len(KERNEL_UNITS) + len(HOST_UNITS), os.cpu_count() or 1))
     lib = LIB_PHASE if phase_clocks else LIB
     extra = ["-DCTCBEAM_PHASE_CLOCKS"] if phase_clocks else []
     with tempfile.TemporaryDirectory(prefix="ctcbeam_build_") as tmp:
@@ -55,9 +56,10 @@ def build(verbose: bool = False, jobs: int = 0, phase_clocks: bool = False) -> s
             o = os.path.join(tmp, unit.replace(".hip", ".o"))
             cmds.append(["hipcc", *COMMON, *extra, *DEVICE, "-c", os.path.join(CSRC, unit), "-o", o])
             objs.append(o)
-        h_o = os.path.join(tmp, "host.o")
-        cmds.append(["hipcc", *COMMON, "-c", os.path.join(CSRC, "ctcbeam_host.cpp"), "-o", h_o])
-        objs.append(h_o)
+        for unit in HOST_UNITS:
+            o = os.path.join(tmp, unit.replace(".cpp", ".o"))
+            cmds.append(["hipcc", *COMMON, "-c", os.path.join(CSRC, unit), "-o", o])
+            objs.append(o)
         with ThreadPoolExecutor(jobs) as ex:
             list(ex.map(_run, cmds))
         out_tmp = lib + f".tmp{os.getpid()}"

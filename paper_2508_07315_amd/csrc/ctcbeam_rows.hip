@@ -1,0 +1,256 @@
+// Row operators, the simple forms: one workgroup per row, the row read from
+// memory for each pass over it.
+#include "ctcbeam_rows_lane.h"
+
+namespace ctcbeam {
+namespace rows {
+
+constexpr int kN = 256;
+constexpr int kSpan = 4096;  // labels whose history counts LDS holds at a time
+
+template <typename T>
+__global__ void __launch_bounds__(kN) process_kernel(const ProcessParams p) {
+  __shared__ uint32_t count[kSpan];
+  __shared__ float red[kN / 64];
+  const int W = p.in.W, tid = threadIdx.x;
+  const int b = blockIdx.x / p.in.T, t = blockIdx.x % p.in.T;
+  if (t >= length_of(p.in, b)) return;
+  const T* x = static_cast<const T*>(p.in.data) + b * p.in.stride_b + t * p.in.stride_t;
+  float* out = p.out + (static_cast<int64_t>(b) * p.in.T + t) * W;
+  const uint32_t* mask = p.mask ? p.mask + b * p.mask_stride_b + t * p.mask_stride_t : nullptr;
+  const float* bias = p.bias ? p.bias + b * p.bias_stride : nullptr;
+  const int32_t* hist = p.history ? p.history + b * p.history_stride : nullptr;
+  int H = hist ? p.H : 0;
+  if (H && p.history_lengths) H = max(0, min(H, p.history_lengths[b]));
+  float rep = p.repetition, pre = p.presence, fre = p.frequency;
+  if (p.penalties) {
+    rep = p.penalties[3 * b];
+    pre = p.penalties[3 * b + 1];
+    fre = p.penalties[3 * b + 2];
+  }
+  float m = kNegInf, s = 0.0f, total = 0.0f;
+  for (int pass = p.normalize ? 0 : 1; pass < 2; ++pass) {
+    for (int c0 = 0; c0 < W; c0 += kSpan) {
+      if (H) {
+        __syncthreads();
+        for (int i = tid; i < kSpan; i += kN) count[i] = 0;
+        __syncthreads();
+        for (int i = tid; i < H; i += kN) {
+          const uint32_t c = static_cast<uint32_t>(hist[i]) - c0;
+          if (hist[i] >= 0 && hist[i] < W && c < kSpan) atomicAdd(&count[c], 1u);
+        }
+        __syncthreads();
+      }
+      for (int c = c0 + tid; c < min(W, c0 + kSpan); c += kN) {
+        float v = clean(to_float(x[c]));
+        const uint32_t n = H ? count[c - c0] : 0;
+        if (n) {
+          v = v > 0.0f ? v / rep : v * rep;
+          v = (v - fre * static_cast<float>(n)) - pre;
+        }
+        if (bias) v += bias[c];
+        v = clean(v);
+        if (mask && !((mask[c >> 5] >> (c & 31)) & 1u)) v = kNegInf;
+        if (pass == 0) {
+          const float mm = fmaxf(m, v);
+          if (mm > kNegInf) s = s * exp2_((m - mm) * kLog2e) + exp2_((v - mm) * kLog2e);
+          m = mm;
+        } else {
+          out[c] = v - total;
+        }
+      }
+    }
+    if (pass == 0) {
+      const float all = block_max<kN>(m, red);
+      const float mine = all > kNegInf ? s * exp2_((m - all) * kLog2e) : 0.0f;
+      s = block_sum<kN>(mine, red);
+      total = all > kNegInf ? all + logf(s) : 0.0f;
+    }
+  }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kN) top_kernel(const TopParams p) {
+  __shared__ float red[kN / 64];
+  __shared__ uint64_t red64[kN / 64];
+  const int W = p.in.W, tid = threadIdx.x;
+  const int b = blockIdx.x / p.in.T, t = blockIdx.x % p.in.T;
+  const int64_t row = static_cast<int64_t>(b) * p.in.T + t;
+  float* values = p.values + row * p.k;
+  int32_t* ids = p.ids + row * p.k;
+  if (t >= length_of(p.in, b)) {
+    for (int i = tid; i < p.k; i += kN) {
+      values[i] = kNegInf;
+      ids[i] = -1;
+    }
+    if (tid == 0) p.tail[row] = kNegInf;
+    return;
+  }
+  const T* x = static_cast<const T*>(p.in.data) + b * p.in.stride_b + t * p.in.stride_t;
+  uint64_t last = ~0ull;
+  for (int i = 0; i < p.k; ++i) {
+    uint64_t best = 0;
+    for (int c = tid; c < W; c += kN) {
+      const uint64_t key = detail::order_key(clean(to_float(x[c])), c);
+      if (key < last && key > best) best = key;
+    }
+    for (int d = 32; d; d >>= 1) {
+      const uint64_t o = __shfl_xor(best, d);
+      best = o > best ? o : best;
+    }
+    __syncthreads();
+    if ((tid & 63) == 0) red64[tid >> 6] = best;
+    __syncthreads();
+    for (int j = 0; j < kN / 64; ++j) best = red64[j] > best ? red64[j] : best;
+    last = best;
+    if (tid == 0) {
+      const int c = static_cast<int>(0xFFFFFFFFu - static_cast<uint32_t>(best));
+      ids[i] = c;
+      values[i] = clean(to_float(x[c]));
+    }
+  }
+  float m = kNegInf, s = 0.0f;
+  for (int c = tid; c < W; c += kN) {
+    const float v = clean(to_float(x[c]));
+    if (detail::order_key(v, c) < last) m = fmaxf(m, v);
+  }
+  m = block_max<kN>(m, red);
+  for (int c = tid; c < W; c += kN) {
+    const float v = clean(to_float(x[c]));
+    if (detail::order_key(v, c) < last && v > kNegInf) s += exp2_((v - m) * p.scale * kLog2e);
+  }
+  s = block_sum<kN>(s, red);
+  if (tid == 0) p.tail[row] = s > 0.0f ? m * p.scale + logf(s) : kNegInf;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kN) distill_kernel(const DistillParams p) {
+  __shared__ uint32_t listed[kMaxLabels / 32];
+  __shared__ int32_t ids[kMaxTop];
+  __shared__ float prob[kMaxTop];
+  __shared__ float red[kN / 64];
+  const int W = p.in.W, tid = threadIdx.x, k = p.k;
+  const int b = blockIdx.x / p.in.T, t = blockIdx.x % p.in.T;
+  const int64_t row = static_cast<int64_t>(b) * p.in.T + t;
+  const T* x = static_cast<const T*>(p.in.data) + b * p.in.stride_b + t * p.in.stride_t;
+  T* grad = p.grad ? static_cast<T*>(p.grad) + b * p.grad_stride_b + t * p.grad_stride_t : nullptr;
+  bool there = t < length_of(p.in, b);
+  float u = kNegInf, rest = kNegInf, m = kNegInf, mr = kNegInf, Z = 0.0f;
+  if (there) {
+    // the teacher's list: P_c = e^u_c / Z, equal labels summed into their first entry
+    int32_t id = -1;
+    if (tid < k) {
+      id = p.ids[row * k + tid];
+      u = clean(p.values[row * k + tid]);
+      u = fminf(u * p.scale, kLargest);
+      if (id < 0 || id >= W || !(u > kNegInf)) {
+        id = -1;
+        u = kNegInf;
+      }
+    }
+    if (p.tail) rest = clean(p.tail[row]);
+    for (int i = tid; i < (W + 31) / 32; i += kN) listed[i] = 0;
+    const float mt = fmaxf(block_max<kN>(u, red), rest);
+    if (mt > kNegInf) {
+      const float e = u > kNegInf ? exp2_((u - mt) * kLog2e) : 0.0f;
+      Z = block_sum<kN>(e, red) + (rest > kNegInf ? exp2_((rest - mt) * kLog2e) : 0.0f);
+      if (tid < k) {
+        ids[tid] = id;
+        prob[tid] = e / Z;
+      }
+      if (id >= 0) atomicOr(&listed[id >> 5], 1u << (id & 31));
+    } else {
+      there = false;
+    }
+    __syncthreads();
+    if (there) {
+      for (int c = tid; c < W; c += kN) {
+        const float v = to_float(x[c]) * p.scale;
+        m = fmaxf(m, v);
+        if (!((listed[c >> 5] >> (c & 31)) & 1u)) mr = fmaxf(mr, v);
+      }
+      m = block_max<kN>(m, red);
+      mr = block_max<kN>(mr, red);
+      float nan = 0.0f;  // a NaN score makes the row's loss and gradient NaN
+      for (int c = tid; c < W; c += kN) {
+        const float v = to_float(x[c]);
+        if (v != v) nan = 1.0f;
+      }
+      nan = block_max<kN>(nan, red);
+      if (nan != 0.0f) m = __builtin_nanf("");
+      if (m == kNegInf) there = false;
+    }
+    if (there) {
+      float s = 0.0f, sr = 0.0f;
+      for (int c = tid; c < W; c += kN) {
+        const float v = to_float(x[c]) * p.scale;
+        s += exp2_((v - m) * kLog2e);
+        if (v > kNegInf && !((listed[c >> 5] >> (c & 31)) & 1u)) sr += exp2_((v - mr) * kLog2e);
+      }
+      s = block_sum<kN>(s, red);
+      sr = block_sum<kN>(sr, red);
+      const float lse = m + logf(s);
+      const float pr = rest > kNegInf ? exp2_((rest - mt) * kLog2e) / Z : 0.0f;
+      float term = 0.0f, P = 0.0f;
+      if (id >= 0) {
+        bool first = true;
+        for (int i = 0; i < k; ++i)
+          if (ids[i] == id) {
+            if (i < tid) first = false;
+            P += prob[i];
+          }
+        if (!first) id = -1;
+      }
+      const float w = (p.weights ? p.weights[b * p.weight_stride_b + t * p.weight_stride_t] : p.weight) * p.scale;
+      if (id >= 0) {
+        const float v = to_float(x[id]) * p.scale;
+        if (P > 0.0f) term = P * (logf(P) - (v - lse));
+        if (grad) from_float((exp2_((v - m) * kLog2e) / s - P) * w, &grad[id]);
+      }
+      if (tid == 0 && pr > 0.0f) term += pr * (rest - mt - logf(Z) - (sr > 0.0f ? mr + logf(sr) - lse : kNegInf));
+      term = block_sum<kN>(term, red);
+      if (p.loss && tid == 0) p.loss[row] = term;
+      if (grad) {
+        const float a = 1.0f / s, c1 = sr > 0.0f ? pr / sr : 0.0f;
+        for (int c = tid; c < W; c += kN) {
+          if ((listed[c >> 5] >> (c & 31)) & 1u) continue;
+          const float v = to_float(x[c]) * p.scale;
+          float g = exp2_((v - m) * kLog2e) * a;
+          if (v > kNegInf) g -= exp2_((v - mr) * kLog2e) * c1;
+          from_float(g * w, &grad[c]);
+        }
+      }
+      return;
+    }
+  }
+  if (p.loss && tid == 0) p.loss[row] = 0.0f;
+  if (grad)
+    for (int c = tid; c < W; c += kN) from_float(0.0f, &grad[c]);
+}
+
+template <typename P, typename F>
+hipError_t by_type(const P& p, F f) {
+  if (p.in.type == kTypeF32) f(float());
+  else if (p.in.type == kTypeF16) f(F16());
+  else f(BF16());
+  return hipGetLastError();
+}
+
+}  // namespace rows
+
+hipError_t launch_process(const ProcessParams& p, hipStream_t stream) {
+  return rows::by_type(p, [&](auto t) {
+    rows::process_kernel<decltype(t)><<<p.in.B * p.in.T, rows::kN, 0, stream>>>(p);
+  });
+}
+hipError_t launch_top(const TopParams& p, hipStream_t stream) {
+  return rows::by_type(p, [&](auto t) {
+    rows::top_kernel<decltype(t)><<<p.in.B * p.in.T, rows::kN, 0, stream>>>(p);
+  });
+}
+hipError_t launch_distill(const DistillParams& p, hipStream_t stream) {
+  return rows::by_type(p, [&](auto t) {
+    rows::distill_kernel<decltype(t)><<<p.in.B * p.in.T, rows::kN, 0, stream>>>(p);
+  });
+}
+}  // namespace ctcbeam

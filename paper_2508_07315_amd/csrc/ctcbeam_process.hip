@@ -1,0 +1,228 @@
+// Penalties for repeated tokens, biases and grammar masks on logits, and the
+// log-softmax that makes the decoders' input of them.
+//
+// A row is read once into registers (as fp32), changed there, and written.
+// What bounds it is memory: W*(sizeof(T) + 4) bytes a row.  Rows of up to
+// kRowOfWave labels belong to a wave, four rows of an utterance to a
+// workgroup; longer ones to a workgroup; rows beyond that, and rows too few to
+// fill the card, are cut into spans of a workgroup each.  With a log-softmax
+// the spans leave (max, sum) in the workspace and a second launch reads them
+// and the scores again (they are still in the caches).
+//
+// The counts of the labels emitted before live in LDS, for the span that the
+// workgroup holds, and serve all its frames.
+#include <algorithm>
+
+#include "ctcbeam_rows_lane.h"
+
+namespace ctcbeam {
+namespace rows {
+
+enum Phase { kWhole = 0, kStats = 1, kFinish = 2 };
+
+struct ProcessPlan {
+  int spans;   // per row
+  int span;    // labels of a span (the last one may hold fewer)
+  int frames;  // per workgroup
+  int groups;  // of frames, per utterance
+};
+
+template <typename T, int N, int F, int PHASE>
+__global__ void __launch_bounds__(kThreads) process_kernel(const ProcessParams p, const ProcessPlan plan, Part* parts) {
+  using L = Layout<T, N, F>;
+  constexpr int V = L::kVec;
+  extern __shared__ uint32_t count[];
+  __shared__ float red[2][N / 64 < 1 ? 1 : N / 64];
+  const int tid = threadIdx.x % N, team = threadIdx.x / N, teams = kThreads / N;
+  const int span = blockIdx.y, b = blockIdx.x / plan.groups;
+  const int t0 = (blockIdx.x % plan.groups) * plan.frames;
+  const int T1 = min(length_of(p.in, b), t0 + plan.frames);
+  if (t0 >= T1) return;
+  const int c0 = span * plan.span;
+  const L lay(min(p.in.W - c0, plan.span), tid);
+  Team<N> tm(red);
+
+  int H = p.H;
+  float rep = 1.0f, pre = 0.0f, fre = 0.0f;
+  if (H) {
+    if (p.history_lengths) H = max(0, min(H, p.history_lengths[b]));
+    rep = p.penalties ? p.penalties[3 * b] : p.repetition;
+    pre = p.penalties ? p.penalties[3 * b + 1] : p.presence;
+    fre = p.penalties ? p.penalties[3 * b + 2] : p.frequency;
+  }
+  if (H) {
+    const int32_t* hist = p.history + b * p.history_stride;
+    for (int i = threadIdx.x; i < lay.W; i += kThreads) count[i] = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < H; i += kThreads) {
+      const uint32_t c = static_cast<uint32_t>(hist[i]) - static_cast<uint32_t>(c0);
+      if (c < static_cast<uint32_t>(lay.W)) atomicAdd(&count[c], 1u);
+    }
+    __syncthreads();
+  }
+  const float* bias = p.bias ? p.bias + b * p.bias_stride + c0 : nullptr;
+
+  for (int t = t0 + team; t < T1; t += teams) {
+    const int64_t row = static_cast<int64_t>(b) * p.in.T + t;
+    const T* in = static_cast<const T*>(p.in.data) + b * p.in.stride_b + t * p.in.stride_t + c0;
+    const uint32_t* mask = p.mask ? p.mask + b * p.mask_stride_b + t * p.mask_stride_t + (c0 >> 5) : nullptr;
+    float x[F + V];
+    lay.load(in, x, kNegInf);
+    const auto seen = [&](float v, uint32_t n) {
+      if (n) {
+        v = v > 0.0f ? v / rep : v * rep;
+        v = clean((v - fre * static_cast<float>(n)) - pre);
+      }
+      return v;
+    };
+    float m = kNegInf;
+#pragma unroll
+    for (int i = 0; i < L::kVecs; ++i)
+      if (i < lay.vecs) {
+        const int c = lay.vec_label(i);
+        float* y = x + i * V;
+#pragma unroll
+        for (int e = 0; e < V; ++e) y[e] = clean(y[e]);
+        if (H) {
+#pragma unroll
+          for (int q = 0; q < V / 4; ++q) {
+            const uint4 n = *reinterpret_cast<const uint4*>(&count[c + 4 * q]);
+            if (n.x | n.y | n.z | n.w) {
+              y[4 * q] = seen(y[4 * q], n.x);
+              y[4 * q + 1] = seen(y[4 * q + 1], n.y);
+              y[4 * q + 2] = seen(y[4 * q + 2], n.z);
+              y[4 * q + 3] = seen(y[4 * q + 3], n.w);
+            }
+          }
+        }
+        if (bias) {
+          float a[V];
+          load_floats<V>(bias + c, a);
+#pragma unroll
+          for (int e = 0; e < V; ++e) y[e] = clean(y[e] + a[e]);
+        }
+        if (mask) {
+          const uint32_t bits = mask[c >> 5] >> (c & 31);
+#pragma unroll
+          for (int e = 0; e < V; ++e) y[e] = (bits >> e) & 1u ? y[e] : kNegInf;
+        }
+#pragma unroll
+        for (int e = 0; e < V; ++e) m = fmaxf(m, y[e]);
+      }
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+      if (j < lay.left && lay.left_label(j) < lay.W) {
+        const int c = lay.left_label(j);
+        float v = clean(x[F + j]);
+        if (H) v = seen(v, count[c]);
+        if (bias) v = clean(v + bias[c]);
+        if (mask && !((mask[c >> 5] >> (c & 31)) & 1u)) v = kNegInf;
+        x[F + j] = v;
+        m = fmaxf(m, v);
+      }
+
+    float total = 0.0f;
+    if (PHASE == kStats || (PHASE == kWhole && p.normalize)) {
+      m = tm.max(m);
+      float s = 0.0f;
+      if (m > kNegInf) {
+        lay.each([&](int e, int) { s += exp2_((x[e] - m) * kLog2e); });
+        s = tm.sum(s);
+        total = m + logf(s);
+      }
+      if (PHASE == kStats) {
+        if (tid == 0) parts[row * plan.spans + span] = {m, s};
+        continue;
+      }
+    }
+    if (PHASE == kFinish) {
+      const Part all = join_parts(parts + row * plan.spans, plan.spans);
+      if (all.m > kNegInf) total = all.m + logf(all.s);
+    }
+    float* out = p.out + row * p.in.W + c0;
+#pragma unroll
+    for (int i = 0; i < L::kVecs; ++i)
+      if (i < lay.vecs) {
+        float y[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) y[e] = x[i * V + e] - total;
+        store_floats<V>(out + lay.vec_label(i), y);
+      }
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+      if (j < lay.left && lay.left_label(j) < lay.W) out[lay.left_label(j)] = x[F + j] - total;
+  }
+}
+
+// Labels of a row that one wave, and one workgroup, take whole: below
+// N * (F + 4), see Layout.
+constexpr int kRowOfWave = 64 * 36, kRowOfGroup = 256 * 36;
+
+static ProcessPlan plan_process(int B, int T, int W, bool normalize, int* n, int* f) {
+  const int64_t rows = static_cast<int64_t>(B) * T;
+  ProcessPlan q{1, W, 1, T};
+  if (W < kRowOfWave && rows >= 1024 && T >= 4) {
+    *n = 64;
+    *f = W < 64 * 20 ? 16 : 32;
+    q.frames = 4;
+  } else if (W < kRowOfGroup && (normalize || rows >= 512)) {
+    *n = 256;
+    *f = W < 256 * 12 ? 8 : W < 256 * 20 ? 16 : 32;
+  } else {
+    // spans: as long as the card stays full of them
+    int span = 8192;
+    while (span > 2048 && rows * ((W + span - 1) / span) < 512) span >>= 1;
+    *n = 256;
+    *f = span / 256;
+    q.spans = (W + span - 1) / span;
+    q.span = span;
+  }
+  // a workgroup's counts of past labels serve several frames where there are enough
+  const int64_t groups = rows * q.spans / q.frames;
+  const int more = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(16, groups / 2048)));
+  q.frames = std::min(q.frames * more, T);
+  q.groups = (T + q.frames - 1) / q.frames;
+  return q;
+}
+
+template <typename T, int N, int F>
+static hipError_t run_process(const ProcessParams& p, const ProcessPlan& q, Part* parts, hipStream_t stream) {
+  const size_t lds = p.H ? sizeof(uint32_t) * ((std::min(q.span, p.in.W) + 3) / 4 * 4) : 0;
+  const dim3 grid(static_cast<uint32_t>(p.in.B) * q.groups, q.spans);
+  if constexpr (N > 64) {
+    if (q.spans > 1 && p.normalize) {
+      process_kernel<T, N, F, kStats><<<grid, kThreads, lds, stream>>>(p, q, parts);
+      process_kernel<T, N, F, kFinish><<<grid, kThreads, lds, stream>>>(p, q, parts);
+      return hipGetLastError();
+    }
+  }
+  process_kernel<T, N, F, kWhole><<<grid, kThreads, lds, stream>>>(p, q, nullptr);
+  return hipGetLastError();
+}
+
+template <typename T>
+static hipError_t choose_process(const ProcessParams& p, const ProcessPlan& q, int n, int f, Part* parts, hipStream_t stream) {
+  if (n == 64) return f == 16 ? run_process<T, 64, 16>(p, q, parts, stream) : run_process<T, 64, 32>(p, q, parts, stream);
+  if (f == 8) return run_process<T, 256, 8>(p, q, parts, stream);
+  if (f == 16) return run_process<T, 256, 16>(p, q, parts, stream);
+  return run_process<T, 256, 32>(p, q, parts, stream);
+}
+
+}  // namespace rows
+
+size_t process_workspace(int B, int T, int W) {
+  int n, f;
+  const rows::ProcessPlan q = rows::plan_process(B, T, W, true, &n, &f);
+  return q.spans == 1 ? 0 : static_cast<size_t>(B) * T * q.spans * sizeof(rows::Part);
+}
+
+hipError_t launch_process(const ProcessParams& p, void* workspace, hipStream_t stream) {
+  int n, f;
+  const rows::ProcessPlan q = rows::plan_process(p.in.B, p.in.T, p.in.W, p.normalize != 0, &n, &f);
+  rows::Part* parts = static_cast<rows::Part*>(workspace);
+  if (p.in.type == kTypeF32) return rows::choose_process<float>(p, q, n, f, parts, stream);
+  if (p.in.type == kTypeF16) return rows::choose_process<rows::F16>(p, q, n, f, parts, stream);
+  return rows::choose_process<rows::BF16>(p, q, n, f, parts, stream);
+}
+
+}  // namespace ctcbeam

@@ -60,7 +60,10 @@ struct DistillParams {
   int64_t grad_stride_b, grad_stride_t;
 };
 
-hipError_t launch_process(const ProcessParams& p, hipStream_t stream);
+// Workspaces in bytes; the launches use no more than these say.
+size_t process_workspace(int B, int T, int W);
+
+hipError_t launch_process(const ProcessParams& p, void* workspace, hipStream_t stream);
 hipError_t launch_top(const TopParams& p, hipStream_t stream);
 hipError_t launch_distill(const DistillParams& p, hipStream_t stream);
 

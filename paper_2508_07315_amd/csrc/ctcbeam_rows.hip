@@ -6,67 +6,26 @@ namespace ctcbeam {
 namespace rows {
 
 constexpr int kN = 256;
-constexpr int kSpan = 4096;  // labels whose history counts LDS holds at a time
 
-template <typename T>
-__global__ void __launch_bounds__(kN) process_kernel(const ProcessParams p) {
-  __shared__ uint32_t count[kSpan];
-  __shared__ float red[kN / 64];
-  const int W = p.in.W, tid = threadIdx.x;
-  const int b = blockIdx.x / p.in.T, t = blockIdx.x % p.in.T;
-  if (t >= length_of(p.in, b)) return;
-  const T* x = static_cast<const T*>(p.in.data) + b * p.in.stride_b + t * p.in.stride_t;
-  float* out = p.out + (static_cast<int64_t>(b) * p.in.T + t) * W;
-  const uint32_t* mask = p.mask ? p.mask + b * p.mask_stride_b + t * p.mask_stride_t : nullptr;
-  const float* bias = p.bias ? p.bias + b * p.bias_stride : nullptr;
-  const int32_t* hist = p.history ? p.history + b * p.history_stride : nullptr;
-  int H = hist ? p.H : 0;
-  if (H && p.history_lengths) H = max(0, min(H, p.history_lengths[b]));
-  float rep = p.repetition, pre = p.presence, fre = p.frequency;
-  if (p.penalties) {
-    rep = p.penalties[3 * b];
-    pre = p.penalties[3 * b + 1];
-    fre = p.penalties[3 * b + 2];
-  }
-  float m = kNegInf, s = 0.0f, total = 0.0f;
-  for (int pass = p.normalize ? 0 : 1; pass < 2; ++pass) {
-    for (int c0 = 0; c0 < W; c0 += kSpan) {
-      if (H) {
-        __syncthreads();
-        for (int i = tid; i < kSpan; i += kN) count[i] = 0;
-        __syncthreads();
-        for (int i = tid; i < H; i += kN) {
-          const uint32_t c = static_cast<uint32_t>(hist[i]) - c0;
-          if (hist[i] >= 0 && hist[i] < W && c < kSpan) atomicAdd(&count[c], 1u);
-        }
-        __syncthreads();
-      }
-      for (int c = c0 + tid; c < min(W, c0 + kSpan); c += kN) {
-        float v = clean(to_float(x[c]));
-        const uint32_t n = H ? count[c - c0] : 0;
-        if (n) {
-          v = v > 0.0f ? v / rep : v * rep;
-          v = (v - fre * static_cast<float>(n)) - pre;
-        }
-        if (bias) v += bias[c];
-        v = clean(v);
-        if (mask && !((mask[c >> 5] >> (c & 31)) & 1u)) v = kNegInf;
-        if (pass == 0) {
-          const float mm = fmaxf(m, v);
-          if (mm > kNegInf) s = s * exp2_((m - mm) * kLog2e) + exp2_((v - mm) * kLog2e);
-          m = mm;
-        } else {
-          out[c] = v - total;
-        }
-      }
-    }
-    if (pass == 0) {
-      const float all = block_max<kN>(m, red);
-      const float mine = all > kNegInf ? s * exp2_((m - all) * kLog2e) : 0.0f;
-      s = block_sum<kN>(mine, red);
-      total = all > kNegInf ? all + logf(s) : 0.0f;
-    }
-  }
+template <int N>
+__device__ __forceinline__ float block_max(float v, float* lds) {
+  v = wave_max(v);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+  __syncthreads();
+  float r = lds[0];
+  for (int i = 1; i < N / 64; ++i) r = fmaxf(r, lds[i]);
+  return r;
+}
+template <int N>
+__device__ __forceinline__ float block_sum(float v, float* lds) {
+  v = wave_sum(v);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+  __syncthreads();
+  float r = lds[0];
+  for (int i = 1; i < N / 64; ++i) r += lds[i];
+  return r;
 }
 
 template <typename T>
@@ -238,11 +197,6 @@ hipError_t by_type(const P& p, F f) {
 
 }  // namespace rows
 
-hipError_t launch_process(const ProcessParams& p, hipStream_t stream) {
-  return rows::by_type(p, [&](auto t) {
-    rows::process_kernel<decltype(t)><<<p.in.B * p.in.T, rows::kN, 0, stream>>>(p);
-  });
-}
 hipError_t launch_top(const TopParams& p, hipStream_t stream) {
   return rows::by_type(p, [&](auto t) {
     rows::top_kernel<decltype(t)><<<p.in.B * p.in.T, rows::kN, 0, stream>>>(p);

@@ -95,6 +95,10 @@ Span rows_span(const ctcbeam_rows* r) {
   return span(r->data, extent(r->B, r->T, r->W, r->stride_b, r->stride_t), element_size(r->type));
 }
 
+bool sizes_fit(int B, int T, int W) {
+  return B > 0 && T > 0 && W > 0 && W <= CTCBEAM_MAX_LABELS && static_cast<Wide>(B) * T <= CTCBEAM_MAX_ROWS;
+}
+
 int device_there() {
   int dev = -1;
   return hipGetDevice(&dev) == hipSuccess ? 0 : refuse(4, "no HIP device");
@@ -105,10 +109,7 @@ int device_there() {
 extern "C" {
 
 size_t ctcbeam_process_workspace_bytes(int B, int T, int W) {
-  (void)B;
-  (void)T;
-  (void)W;
-  return 0;
+  return sizes_fit(B, T, W) ? ctcbeam::process_workspace(B, T, W) : 0;
 }
 
 size_t ctcbeam_top_workspace_bytes(int B, int T, int W, int k) {
@@ -163,6 +164,8 @@ int ctcbeam_process_logits(const ctcbeam_rows* logits, const ctcbeam_process_opt
   if (workspace_bytes < ctcbeam_process_workspace_bytes(B, T, W) ||
       (!workspace && ctcbeam_process_workspace_bytes(B, T, W) > 0))
     return refuse(1, "workspace too small");
+  if (misaligned(workspace, 16)) return refuse(1, "workspace is not aligned to 16 bytes");
+  if (meet_any(span(workspace, static_cast<Wide>(workspace_bytes), 1), {so, si})) return refuse(1, "workspace overlaps another argument");
   if (int rc = device_there()) return rc;
   ctcbeam::ProcessParams p{};
   p.in = view(logits);
@@ -183,7 +186,7 @@ int ctcbeam_process_logits(const ctcbeam_rows* logits, const ctcbeam_process_opt
   p.mask_stride_t = o.mask_stride_t;
   p.normalize = o.normalize != 0;
   p.out = out;
-  return launched(ctcbeam::launch_process(p, stream));
+  return launched(ctcbeam::launch_process(p, workspace, stream));
 }
 
 int ctcbeam_top_logits(const ctcbeam_rows* logits, int k, float temperature, float* values, int32_t* ids, float* tail,

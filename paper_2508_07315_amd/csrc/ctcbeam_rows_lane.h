@@ -1,6 +1,8 @@
-// Device helpers of the row operators: element access, sums and maxima over a
-// workgroup, and the treatment of values that are no number.
+// Device side of the row operators: a row held in registers, sums and maxima
+// over the threads of a row, and the treatment of values that are no number.
 #pragma once
+
+#include <type_traits>
 
 #include "ctcbeam_lane.h"
 #include "ctcbeam_rows.h"
@@ -8,6 +10,7 @@
 namespace ctcbeam {
 namespace rows {
 
+constexpr int kThreads = 256;  // per workgroup
 constexpr float kNegInf = -__builtin_huge_valf();
 constexpr float kLargest = 3.402823466e38f;
 constexpr float kLog2e = 1.4426950408889634f;
@@ -19,40 +22,190 @@ struct BF16 { uint16_t u; };
 __device__ __forceinline__ float to_float(float v) { return v; }
 __device__ __forceinline__ float to_float(F16 v) { return static_cast<float>(__builtin_bit_cast(_Float16, v.u)); }
 __device__ __forceinline__ float to_float(BF16 v) { return __uint_as_float(static_cast<uint32_t>(v.u) << 16); }
+// one rounding, to nearest even
 __device__ __forceinline__ void from_float(float v, float* o) { *o = v; }
 __device__ __forceinline__ void from_float(float v, F16* o) { o->u = __builtin_bit_cast(uint16_t, static_cast<_Float16>(v)); }
 __device__ __forceinline__ void from_float(float v, BF16* o) { o->u = __builtin_bit_cast(uint16_t, static_cast<__bf16>(v)); }
 
 // NaN counts as -inf, +inf as the largest number
-__device__ __forceinline__ float clean(float v) { return v != v ? kNegInf : fminf(v, kLargest); }
+__device__ __forceinline__ float clean(float v) { return fminf(fmaxf(v, kNegInf), kLargest); }
 
 __device__ __forceinline__ float exp2_(float v) { return __builtin_amdgcn_exp2f(v); }
 
-template <int N>
-__device__ __forceinline__ float block_max(float v, float* lds) {
-  for (int d = 32; d; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
-  __syncthreads();
-  float r = lds[0];
-  for (int i = 1; i < N / 64; ++i) r = fmaxf(r, lds[i]);
-  return r;
+// 16 bytes at any address: rows of an odd number of labels start anywhere.
+struct __attribute__((packed, aligned(2))) Bytes16 { uint32_t w[4]; };
+struct __attribute__((packed, aligned(4))) Floats4 { float f[4]; };
+
+template <typename T>
+struct Packed {
+  static constexpr int kVec = 16 / static_cast<int>(sizeof(T));
+};
+__device__ __forceinline__ void unpack(const Bytes16& b, float* o, float) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) o[i] = __uint_as_float(b.w[i]);
 }
+__device__ __forceinline__ void unpack(const Bytes16& b, float* o, F16) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    o[2 * i] = to_float(F16{static_cast<uint16_t>(b.w[i])});
+    o[2 * i + 1] = to_float(F16{static_cast<uint16_t>(b.w[i] >> 16)});
+  }
+}
+__device__ __forceinline__ void unpack(const Bytes16& b, float* o, BF16) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    o[2 * i] = __uint_as_float(b.w[i] << 16);
+    o[2 * i + 1] = __uint_as_float(b.w[i] & 0xFFFF0000u);
+  }
+}
+
+// ---- over a wave: every lane gets the result, and the same bits of it ----
+template <typename Op>
+__device__ __forceinline__ float wave_join(float v, Op op) {
+  const auto dpp = [](float x, auto ctrl) {
+    return __uint_as_float(detail::dpp_full<decltype(ctrl)::value>(__float_as_uint(x)));
+  };
+  v = op(v, dpp(v, std::integral_constant<int, detail::kDppQuadXor1>{}));
+  v = op(v, dpp(v, std::integral_constant<int, detail::kDppQuadXor2>{}));
+  v = op(v, dpp(v, std::integral_constant<int, 0x141>{}));  // mirrored within 8 lanes
+  v = op(v, dpp(v, std::integral_constant<int, 0x140>{}));  // mirrored within 16
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = op(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return op(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+struct Max {
+  __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }
+};
+struct Sum {
+  __device__ __forceinline__ float operator()(float a, float b) const { return a + b; }
+};
+__device__ __forceinline__ float wave_max(float v) { return wave_join(v, Max()); }
+__device__ __forceinline__ float wave_sum(float v) { return wave_join(v, Sum()); }
+
+// ---- over the N threads of a row: a wave, or the whole workgroup ----
+// Consecutive calls use the two halves of `lds` in turn, so one barrier a call
+// is enough.
 template <int N>
-__device__ __forceinline__ float block_sum(float v, float* lds) {
-  for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
-  __syncthreads();
-  float r = lds[0];
-  for (int i = 1; i < N / 64; ++i) r += lds[i];
-  return r;
+struct Team {
+  float (*lds)[N / 64];
+  int turn = 0;
+  __device__ __forceinline__ explicit Team(float (*l)[N / 64]) : lds(l) {}
+  template <typename Op>
+  __device__ __forceinline__ float join(float v, Op op) {
+    v = wave_join(v, op);
+    if constexpr (N > 64) {
+      if ((threadIdx.x & 63) == 0) lds[turn][threadIdx.x >> 6] = v;
+      __syncthreads();
+      v = lds[turn][0];
+#pragma unroll
+      for (int i = 1; i < N / 64; ++i) v = op(v, lds[turn][i]);
+      turn ^= 1;
+    }
+    return v;
+  }
+  __device__ __forceinline__ float max(float v) { return join(v, Max()); }
+  __device__ __forceinline__ float sum(float v) { return join(v, Sum()); }
+  __device__ __forceinline__ void sync() {
+    if constexpr (N > 64) __syncthreads();
+    else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  }
+};
+
+// The labels of a row (or of a span of it), spread over N threads: first whole
+// vectors of 16 bytes a thread, i-th vector at label (i*N + tid)*kVec, then
+// what is left label by label, j-th at base + j*N + tid.  An odd number of
+// labels costs one load more, not a half-empty vector.
+template <typename T, int N, int F>
+struct Layout {
+  static constexpr int kVec = Packed<T>::kVec, kVecs = F / kVec, kSpan = N * F, kMost = N * (F + kVec) - 1;
+  int W, tid, vecs, base, left;
+  __device__ __forceinline__ Layout(int w, int t) : W(w), tid(t) {
+    vecs = w / (N * kVec);
+    base = vecs * N * kVec;
+    left = (w - base + N - 1) / N;
+  }
+  __device__ __forceinline__ int vec_label(int i) const { return (i * N + tid) * kVec; }
+  __device__ __forceinline__ int left_label(int j) const { return base + j * N + tid; }
+  // f(e, label, value index) for every label of this thread
+  template <typename Fn>
+  __device__ __forceinline__ void each(Fn f) const {
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i)
+      if (i < vecs) {
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) f(i * kVec + e, vec_label(i) + e);
+      }
+#pragma unroll
+    for (int j = 0; j < kVec; ++j)
+      if (j < left && left_label(j) < W) f(F + j, left_label(j));
+  }
+  // x[0 .. F+kVec): the row's scores as fp32; `fill` where there is no label
+  __device__ __forceinline__ void load(const T* row, float* x, float fill) const {
+    Bytes16 raw[kVecs];
+    T one[kVec];
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i)
+      if (i < vecs) raw[i] = *reinterpret_cast<const Bytes16*>(row + vec_label(i));
+#pragma unroll
+    for (int j = 0; j < kVec; ++j)
+      if (j < left && left_label(j) < W) one[j] = row[left_label(j)];
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+      if (i < vecs) {
+        unpack(raw[i], x + i * kVec, T());
+      } else {
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) x[i * kVec + e] = fill;
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) x[F + j] = j < left && left_label(j) < W ? to_float(one[j]) : fill;
+  }
+};
+
+// kVec fp32 values at an address of 4-byte alignment
+template <int V>
+__device__ __forceinline__ void load_floats(const float* p, float* o) {
+#pragma unroll
+  for (int i = 0; i < V / 4; ++i) {
+    const Floats4 f = reinterpret_cast<const Floats4*>(p)[i];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[4 * i + e] = f.f[e];
+  }
+}
+template <int V>
+__device__ __forceinline__ void store_floats(float* p, const float* v) {
+#pragma unroll
+  for (int i = 0; i < V / 4; ++i) {
+    Floats4 f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f.f[e] = v[4 * i + e];
+    reinterpret_cast<Floats4*>(p)[i] = f;
+  }
 }
 
 __device__ __forceinline__ int length_of(const RowsView& v, int b) {
   if (!v.lengths) return v.T;
   const int l = v.lengths[b];
   return l < 0 ? 0 : (l > v.T ? v.T : l);
+}
+
+// A maximum and a sum of exp2((x - max) * log2 e) of parts of a row, as the
+// parts leave them in a workspace.
+struct Part {
+  float m, s;
+};
+__device__ __forceinline__ Part join_parts(const Part* parts, int n) {
+  const int lane = threadIdx.x & 63;
+  float m = kNegInf, s = 0.0f;
+  for (int i = lane; i < n; i += 64) m = fmaxf(m, parts[i].m);
+  m = wave_max(m);
+  for (int i = lane; i < n; i += 64) {
+    const Part p = parts[i];
+    if (p.m > kNegInf) s += p.s * exp2_((p.m - m) * kLog2e);
+  }
+  return {m, wave_sum(s)};
 }
 
 }  // namespace rows

@@ -29,60 +29,6 @@ __device__ __forceinline__ float block_sum(float v, float* lds) {
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kN) top_kernel(const TopParams p) {
-  __shared__ float red[kN / 64];
-  __shared__ uint64_t red64[kN / 64];
-  const int W = p.in.W, tid = threadIdx.x;
-  const int b = blockIdx.x / p.in.T, t = blockIdx.x % p.in.T;
-  const int64_t row = static_cast<int64_t>(b) * p.in.T + t;
-  float* values = p.values + row * p.k;
-  int32_t* ids = p.ids + row * p.k;
-  if (t >= length_of(p.in, b)) {
-    for (int i = tid; i < p.k; i += kN) {
-      values[i] = kNegInf;
-      ids[i] = -1;
-    }
-    if (tid == 0) p.tail[row] = kNegInf;
-    return;
-  }
-  const T* x = static_cast<const T*>(p.in.data) + b * p.in.stride_b + t * p.in.stride_t;
-  uint64_t last = ~0ull;
-  for (int i = 0; i < p.k; ++i) {
-    uint64_t best = 0;
-    for (int c = tid; c < W; c += kN) {
-      const uint64_t key = detail::order_key(clean(to_float(x[c])), c);
-      if (key < last && key > best) best = key;
-    }
-    for (int d = 32; d; d >>= 1) {
-      const uint64_t o = __shfl_xor(best, d);
-      best = o > best ? o : best;
-    }
-    __syncthreads();
-    if ((tid & 63) == 0) red64[tid >> 6] = best;
-    __syncthreads();
-    for (int j = 0; j < kN / 64; ++j) best = red64[j] > best ? red64[j] : best;
-    last = best;
-    if (tid == 0) {
-      const int c = static_cast<int>(0xFFFFFFFFu - static_cast<uint32_t>(best));
-      ids[i] = c;
-      values[i] = clean(to_float(x[c]));
-    }
-  }
-  float m = kNegInf, s = 0.0f;
-  for (int c = tid; c < W; c += kN) {
-    const float v = clean(to_float(x[c]));
-    if (detail::order_key(v, c) < last) m = fmaxf(m, v);
-  }
-  m = block_max<kN>(m, red);
-  for (int c = tid; c < W; c += kN) {
-    const float v = clean(to_float(x[c]));
-    if (detail::order_key(v, c) < last && v > kNegInf) s += exp2_((v - m) * p.scale * kLog2e);
-  }
-  s = block_sum<kN>(s, red);
-  if (tid == 0) p.tail[row] = s > 0.0f ? m * p.scale + logf(s) : kNegInf;
-}
-
-template <typename T>
 __global__ void __launch_bounds__(kN) distill_kernel(const DistillParams p) {
   __shared__ uint32_t listed[kMaxLabels / 32];
   __shared__ int32_t ids[kMaxTop];
@@ -197,11 +143,6 @@ hipError_t by_type(const P& p, F f) {
 
 }  // namespace rows
 
-hipError_t launch_top(const TopParams& p, hipStream_t stream) {
-  return rows::by_type(p, [&](auto t) {
-    rows::top_kernel<decltype(t)><<<p.in.B * p.in.T, rows::kN, 0, stream>>>(p);
-  });
-}
 hipError_t launch_distill(const DistillParams& p, hipStream_t stream) {
   return rows::by_type(p, [&](auto t) {
     rows::distill_kernel<decltype(t)><<<p.in.B * p.in.T, rows::kN, 0, stream>>>(p);

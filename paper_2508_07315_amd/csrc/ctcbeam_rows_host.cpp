@@ -113,11 +113,7 @@ size_t ctcbeam_process_workspace_bytes(int B, int T, int W) {
 }
 
 size_t ctcbeam_top_workspace_bytes(int B, int T, int W, int k) {
-  (void)B;
-  (void)T;
-  (void)W;
-  (void)k;
-  return 0;
+  return sizes_fit(B, T, W) && k > 0 && k <= CTCBEAM_MAX_TOP ? ctcbeam::top_workspace(B, T, W, k) : 0;
 }
 
 size_t ctcbeam_distill_workspace_bytes(int B, int T, int W) {
@@ -212,6 +208,9 @@ int ctcbeam_top_logits(const ctcbeam_rows* logits, int k, float temperature, flo
   if (workspace_bytes < ctcbeam_top_workspace_bytes(B, T, W, k) ||
       (!workspace && ctcbeam_top_workspace_bytes(B, T, W, k) > 0))
     return refuse(1, "workspace too small");
+  if (misaligned(workspace, 16)) return refuse(1, "workspace is not aligned to 16 bytes");
+  if (meet_any(span(workspace, static_cast<Wide>(workspace_bytes), 1), {sv, si, st, sx, sl}))
+    return refuse(1, "workspace overlaps another argument");
   if (int rc = device_there()) return rc;
   ctcbeam::TopParams p{};
   p.in = view(logits);
@@ -220,7 +219,7 @@ int ctcbeam_top_logits(const ctcbeam_rows* logits, int k, float temperature, flo
   p.values = values;
   p.ids = ids;
   p.tail = tail;
-  return launched(ctcbeam::launch_top(p, stream));
+  return launched(ctcbeam::launch_top(p, workspace, stream));
 }
 
 int ctcbeam_distill(const ctcbeam_rows* student, const float* top_values, const int32_t* top_ids, const float* tail, int k,

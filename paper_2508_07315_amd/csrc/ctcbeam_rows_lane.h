@@ -164,6 +164,52 @@ struct Layout {
   }
 };
 
+// A row as it was read; each pass over it unpacks it again.
+template <typename T, int N, int F>
+struct RawRow {
+  using L = Layout<T, N, F>;
+  Bytes16 raw[L::kVecs] = {};
+  T one[L::kVec] = {};
+  __device__ __forceinline__ RawRow(const L& lay, const T* row) {
+#pragma unroll
+    for (int i = 0; i < L::kVecs; ++i)
+      if (i < lay.vecs) raw[i] = *reinterpret_cast<const Bytes16*>(row + lay.vec_label(i));
+#pragma unroll
+    for (int j = 0; j < L::kVec; ++j)
+      if (j < lay.left && lay.left_label(j) < lay.W) one[j] = row[lay.left_label(j)];
+  }
+  // f(value, label, there) for the labels of this thread, by all threads alike:
+  // `there` is false behind the last label
+  template <typename Fn>
+  __device__ __forceinline__ void every(const L& lay, Fn f) const {
+#pragma unroll
+    for (int i = 0; i < L::kVecs; ++i)
+      if (i < lay.vecs) {
+        float v[L::kVec];
+        unpack(raw[i], v, T());
+#pragma unroll
+        for (int e = 0; e < L::kVec; ++e) f(v[e], lay.vec_label(i) + e, true);
+      }
+#pragma unroll
+    for (int j = 0; j < L::kVec; ++j)
+      if (j < lay.left) f(to_float(one[j]), lay.left_label(j), lay.left_label(j) < lay.W);
+  }
+  template <typename Fn>
+  __device__ __forceinline__ void each(const L& lay, Fn f) const {
+    every(lay, [&](float v, int label, bool there) {
+      if (there) f(v, label);
+    });
+  }
+  // What follows unpacks the row anew, instead of keeping unpacked (or
+  // otherwise derived) values of all labels in registers from before.
+  __device__ __forceinline__ void forget() {
+#pragma unroll
+    for (int i = 0; i < L::kVecs; ++i)
+#pragma unroll
+      for (int w = 0; w < 4; ++w) asm volatile("" : "+v"(raw[i].w[w]));
+  }
+};
+
 // kVec fp32 values at an address of 4-byte alignment
 template <int V>
 __device__ __forceinline__ void load_floats(const float* p, float* o) {

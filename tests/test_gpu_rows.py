@@ -204,6 +204,23 @@ def test_top_sizes(B, T, W, k):
     top_case(scores(B, T, W, "bf16", W + k), k, what=f"B={B} T={T} W={W} k={k}")
 
 
+@pytest.mark.parametrize("W,k", [(33, 32), (64, 1), (1025, 16), (1279, 32), (1280, 5), (2303, 32), (2304, 7)])
+@pytest.mark.parametrize("kind", KINDS)
+def test_top_many_rows(W, k, kind):
+    """Enough rows for the form that gives each a wave, with rows of ties, of nothing and of a far tail among them."""
+    x = torch.randn((9, 130, W), generator=gen(W)) * 2.0
+    c = torch.arange(W).float()
+    x[1, :, :] = (c % 7 == 3).float()
+    x[2, 5], x[2, 6] = -INF, -INF
+    x[2, 6, W // 2] = 1.0
+    x[3, 7] = c // 40
+    x[3, 8] = math.nan
+    x[3, 9, ::2] = math.nan
+    x[3, 10] = -500.0
+    x[3, 10, W // 3] = 500.0
+    top_case(x.to(R.TYPES[kind]).to(dev()), k, [130, 7, 100, 130, 0, 1, 130, 129, 64], 2.0, f"W={W} k={k} {kind}")
+
+
 def test_top_tail_far_below():
     """What is left may lie far below the list: its log-sum stays finite."""
     x = torch.full((1, 2, 900), -300.0)
@@ -253,14 +270,18 @@ def test_distill_widths(i, W, kind):
                      pick(i + j, [None, [T, 0, T + 4][:B], [2, -1, 1][:B]]), temperature, w, f"W={W} k={k} {kind}", kind)
 
 
-@pytest.mark.parametrize("B,T,W,k", [(1, 1, 262144, 128), (260, 1, 700, 4), (1, 300, 1025, 16), (30, 1, 20001, 50)])
+@pytest.mark.parametrize("B,T,W,k", [(1, 1, 262144, 128), (260, 1, 700, 4), (1, 300, 1025, 16), (30, 1, 20001, 50),
+                                     (300, 4, 33, 5), (2, 520, 1025, 128), (1030, 1, 2303, 16)])
 def test_distill_sizes(B, T, W, k):
     v, ids, tail = teacher(B, T, W, k, W)
     distill_case(scores(B, T, W, "bf16", W + 1), v, ids, tail, what=f"B={B} T={T} W={W}", kind="bf16")
 
 
-@pytest.mark.parametrize("W", [50, 1025, 6000, 90000])
-def test_distill_odd_lists(W):
+ODD_ROWS = [(50, 1), (1025, 1), (1025, 130), (2303, 130), (6000, 1), (90000, 1)]   # labels, times the 8 rows
+
+
+@pytest.mark.parametrize("W,times", ODD_ROWS)
+def test_distill_odd_lists(W, times):
     """Ids twice and three times, ids out of range, empty lists, values of -inf and NaN, all of the mass in the tail."""
     x = scores(8, 1, W, "fp32", W)
     v, ids, tail = teacher(8, 1, W, 6, W + 1)
@@ -272,12 +293,13 @@ def test_distill_odd_lists(W):
     v[5, 0] = -INF
     v[6, 0], tail[6, 0] = -200.0, 0.0                 # the list holds next to nothing
     tail[7, 0] = -INF
+    x, v, ids, tail = (a.repeat(times, *[1] * (a.dim() - 1)) for a in (x, v, ids, tail))
     loss, grad = distill_case(x, v, ids, tail, what=f"W={W}")
     assert loss[3, 0] == 0 and (grad[3] == 0).all()
 
 
-@pytest.mark.parametrize("W", [50, 1025, 6000, 90000])
-def test_distill_odd_students(W):
+@pytest.mark.parametrize("W,times", ODD_ROWS)
+def test_distill_odd_students(W, times):
     """Barred labels, rows of -inf, peaks that leave the rest far below, NaN and +inf."""
     x = scores(8, 1, W, "fp32", W)
     v, ids, tail = teacher(8, 1, W, 6, W + 1)
@@ -291,6 +313,7 @@ def test_distill_odd_students(W):
     x[5, 0, W // 2] = math.nan
     x[6, 0, W // 2] = INF
     x[7, 0, :W // 2] = -INF
+    x, v, ids, tail = (a.repeat(times, *[1] * (a.dim() - 1)) for a in (x, v, ids, tail))
     loss, grad = distill_case(x, v, ids, tail, what=f"W={W}")
     assert (loss[0] == 0).all() and (grad[0] == 0).all()
     assert loss[1, 0] == INF and torch.isfinite(grad[1]).all()

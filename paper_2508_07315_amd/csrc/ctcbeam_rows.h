@@ -63,9 +63,10 @@ struct DistillParams {
 // Workspaces in bytes; the launches use no more than these say.
 size_t process_workspace(int B, int T, int W);
 size_t top_workspace(int B, int T, int W, int k);
+size_t distill_workspace(int B, int T, int W);
 
 hipError_t launch_process(const ProcessParams& p, void* workspace, hipStream_t stream);
 hipError_t launch_top(const TopParams& p, void* workspace, hipStream_t stream);
-hipError_t launch_distill(const DistillParams& p, hipStream_t stream);
+hipError_t launch_distill(const DistillParams& p, void* workspace, hipStream_t stream);
 
 }  // namespace ctcbeam

@@ -117,10 +117,7 @@ size_t ctcbeam_top_workspace_bytes(int B, int T, int W, int k) {
 }
 
 size_t ctcbeam_distill_workspace_bytes(int B, int T, int W) {
-  (void)B;
-  (void)T;
-  (void)W;
-  return 0;
+  return sizes_fit(B, T, W) ? ctcbeam::distill_workspace(B, T, W) : 0;
 }
 
 int ctcbeam_process_logits(const ctcbeam_rows* logits, const ctcbeam_process_opts* opts, float* out, void* workspace,
@@ -262,6 +259,9 @@ int ctcbeam_distill(const ctcbeam_rows* student, const float* top_values, const 
   if (workspace_bytes < ctcbeam_distill_workspace_bytes(B, T, W) ||
       (!workspace && ctcbeam_distill_workspace_bytes(B, T, W) > 0))
     return refuse(1, "workspace too small");
+  if (misaligned(workspace, 16)) return refuse(1, "workspace is not aligned to 16 bytes");
+  if (meet_any(span(workspace, static_cast<Wide>(workspace_bytes), 1), {sl, sg, sx, sn, sv, si, st, sw}))
+    return refuse(1, "workspace overlaps another argument");
   if (int rc = device_there()) return rc;
   ctcbeam::DistillParams p{};
   p.in = view(student);
@@ -278,7 +278,7 @@ int ctcbeam_distill(const ctcbeam_rows* student, const float* top_values, const 
   p.grad = grad;
   p.grad_stride_b = grad_stride_b;
   p.grad_stride_t = grad_stride_t;
-  return launched(ctcbeam::launch_distill(p, stream));
+  return launched(ctcbeam::launch_distill(p, workspace, stream));
 }
 
 }  // extern "C"

@@ -2,24 +2,25 @@
 // its gradient, in one pass over the student's row.
 //
 //   Z = sum_i exp(u_i) + exp(tail), P_c = sum_(i of c) exp(u_i) / Z, P_r = exp(tail) / Z
-//   e_c = exp(s (x_c - m)), S = sum e_c, R = sum of e_c over the labels that are not listed
-//   loss = sum_c P_c (log P_c - log e_c + log S) + P_r (log P_r - log R + log S)
-//   grad_c = w s (e_c / S - P_c) where listed, w s e_c (1 / S - P_r / R) elsewhere
+//   r, m: the largest score of the labels that are not listed, and of all
+//   R = sum over the labels that are not listed of e_c, e_c = exp(s (x_c - r))
+//   S = R exp(s (r - m)) + sum over the listed labels of exp(s (x_c - m))
+//   loss = sum_c P_c (log P_c - s (x_c - m) + log S) + P_r (log P_r - s (r - m) - log R + log S)
+//   grad_c = w s (exp(s (x_c - m)) / S - P_c) where listed,
+//            w s (exp(s (r - m)) / S - P_r / R) e_c elsewhere
 //
-// R is a sum of its own, never S less the listed labels, and where it is too
-// small for fp32 beside m it is taken again relative to its own maximum, so
-// neither the loss nor the gradient cancels.
+// The listed labels are taken out of the row (set to -inf) as soon as it is
+// there, and come back as they are written.  So the passes over the row know
+// nothing of the list, R is a sum of its own at its own scale, never S less the
+// listed labels, and neither the loss nor the gradient cancels.
 //
-// The row is read once into registers.  The teacher's probabilities are
-// scattered to a table in LDS with a place for every label of the span, which
-// both passes over the registers read beside them: whether a label is listed,
-// and what to take from its gradient.  Labels listed twice are found by the
-// scatter itself and summed in the order of the list.
-//
-// What bounds it is memory: the row in and the gradient out.  A wave takes
-// rows of fewer than 2304 labels where there are many, a workgroup rows of
-// fewer than 9216; longer ones are cut into spans whose sums a second launch
-// joins, reading the row again for the gradient.
+// What bounds it is memory, the row in and the gradient out, and for 16-bit
+// rows nearly as much the exponentials and conversions.  A wave takes rows of
+// fewer than 2304 labels where there are many, a workgroup of 256 rows of
+// fewer than 9216, through a copy of the row in LDS in which the list is taken
+// out and put back.  Longer rows are held by a workgroup of 1024, in packed
+// registers, with a bit per label in LDS; or, where they are few or longer than
+// that, cut into spans whose sums a second launch joins.
 #include <algorithm>
 
 #include "ctcbeam_rows_lane.h"
@@ -35,220 +36,221 @@ struct DistillPlan {
   int span;   // labels of a span (the last one may hold fewer)
 };
 
-// What a span leaves for the second launch: m and S; R relative to r; the
-// listed labels' part of the loss but for log S, and their probability.
+// What a span leaves for the second launch: the sum over its listed labels
+// relative to m, R relative to r, the listed labels' part of the loss but for
+// log S, and their probability.
 struct SpanSums {
-  float m, S, r, R, terms, listed;
+  float m, listed_sum, r, R, terms, listed;
 };
 
-constexpr float kSmallRest = 0x1p-80f;      // R below this is taken again relative to its own maximum
-constexpr float kListed = 1.17549435e-38f;  // least table entry of a listed label
+// The teacher's list of a row, two entries a lane.
+struct List {
+  int id[2];  // label within the span, -1: no entry of this span
+  float prob[2], log_prob[2], score[2];
+  float rest_p, log_rest_p;
+  bool any, two;  // more than 64 entries: the lanes' second ones
 
-__device__ __forceinline__ void store_vec(float* p, const float* v) { store_floats<4>(p, v); }
-template <typename T>
-__device__ __forceinline__ void store_vec(T* p, const float* v) {
-  Bytes16 b;
+  __device__ __forceinline__ List(const DistillParams& p, int64_t row, int c0, int W) {
+    const int lane = threadIdx.x & 63;
+    two = p.k > 64;
+    float u[2];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    T lo, hi;
-    from_float(v[2 * i], &lo);
-    from_float(v[2 * i + 1], &hi);
-    b.w[i] = static_cast<uint32_t>(lo.u) | (static_cast<uint32_t>(hi.u) << 16);
+    for (int e = 0; e < 2; ++e) {
+      const int i = lane + 64 * e;
+      u[e] = kNegInf;
+      id[e] = -1;
+      prob[e] = log_prob[e] = score[e] = 0.0f;
+      if (e == 1 && !two) break;
+      if (i < p.k) {
+        const int at = p.ids[row * p.k + i];
+        const float v = clean(p.values[row * p.k + i]);
+        if (at >= 0 && at < p.in.W && v > kNegInf) {
+          id[e] = at - c0;
+          u[e] = fminf(v * p.scale, kLargest);
+        }
+      }
+      if (id[e] >= W) id[e] = -1;
+    }
+    const float rest = p.tail ? clean(p.tail[row]) : kNegInf;
+    const float mt = fmaxf(wave_max(fmaxf(u[0], u[1])), rest);
+    any = mt > kNegInf;
+    const float m0 = any ? mt : 0.0f;
+    each([&](int e) { prob[e] = exp2_((u[e] - m0) * kLog2e); });
+    const float rest_e = exp2_((rest - m0) * kLog2e), Z = wave_sum(prob[0] + prob[1]) + rest_e;
+    const float log_z = log_(Z), per_z = rcp_(Z);
+    rest_p = rest_e * per_z;
+    log_rest_p = (rest - m0) - log_z;
+    each([&](int e) {
+      prob[e] *= per_z;
+      log_prob[e] = (u[e] - m0) - log_z;
+    });
   }
-  *reinterpret_cast<Bytes16*>(p) = b;
+
+  template <typename Fn>
+  __device__ __forceinline__ void each(Fn f) const {
+    f(0);
+    if (two) f(1);
+  }
+
+  // Labels listed more than once: their first entry takes the sum, in the
+  // list's order, the others are no entries.
+  __device__ __forceinline__ void sum_equal_labels(int k) {
+    const int lane = threadIdx.x & 63;
+    float sum[2] = {0.0f, 0.0f};
+    bool first[2] = {true, true};
+    for (int i = 0; i < k; ++i) {
+      const int other = i < 64 ? __shfl(id[0], i) : __shfl(id[1], i - 64);
+      const float more = i < 64 ? __shfl(prob[0], i) : __shfl(prob[1], i - 64);
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+        if (other == id[e]) {
+          sum[e] += more;
+          if (i < lane + 64 * e) first[e] = false;
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      if (id[e] < 0) continue;
+      prob[e] = sum[e];
+      log_prob[e] = logf(sum[e]);
+      if (!first[e]) id[e] = -1;
+    }
+  }
+
+  __device__ __forceinline__ float largest() const {
+    return fmaxf(id[0] >= 0 ? score[0] : kNegInf, id[1] >= 0 ? score[1] : kNegInf);
+  }
+  // the listed labels' sum relative to m
+  __device__ __forceinline__ float sum(float m, float c) const {
+    float s = 0.0f;
+    each([&](int e) {
+      if (id[e] >= 0) s += exp2_((score[e] - m) * c);
+    });
+    return s;
+  }
+  // their part of the loss but for log S
+  __device__ __forceinline__ float terms(float m, float scale) const {
+    float t = 0.0f;
+    each([&](int e) {
+      if (id[e] >= 0 && prob[e] > 0.0f) t += prob[e] * (log_prob[e] - (score[e] - m) * scale);
+    });
+    return t;
+  }
+  __device__ __forceinline__ float listed() const {
+    return (id[0] >= 0 ? prob[0] : 0.0f) + (id[1] >= 0 ? prob[1] : 0.0f);
+  }
+};
+
+// What the sums of a row make: its loss, from the listed labels' part of it,
+// and the factors of the gradient.
+struct RowSums {
+  float m, r, R, S;
+  __device__ __forceinline__ RowSums(float m_, float r_, float R_, float listed_sum, float c) : m(m_), r(r_), R(R_) {
+    // (with nothing above -inf, R is 0, or NaN where a score is)
+    S = (r > kNegInf ? R * exp2_((r - m) * c) : R) + listed_sum;
+  }
+  // the part of the loss of the labels that are not listed
+  __device__ __forceinline__ float rest_loss(const List& list, float scale) const {
+    if (!(list.rest_p > 0.0f)) return 0.0f;
+    const float log_q = R > 0.0f ? (r - m) * scale + log_(R) - log_(S) : S != S ? S : kNegInf;
+    return list.rest_p * (list.log_rest_p - log_q);
+  }
+  __device__ __forceinline__ float listed_factor(float w) const { return w * rcp_(S); }
+  __device__ __forceinline__ float rest_factor(float w, float c, const List& list) const {
+    return (r > kNegInf ? exp2_((r - m) * c) : 0.0f) * (w * rcp_(S)) - (R > 0.0f ? w * list.rest_p * rcp_(R) : 0.0f);
+  }
+};
+
+__device__ __forceinline__ float row_weight(const DistillParams& p, int b, int t) {
+  return (p.weights ? p.weights[b * p.weight_stride_b + t * p.weight_stride_t] : p.weight) * p.scale;
 }
 
+// Loss 0 and gradient 0.
+template <typename T, int N, int F>
+__device__ __forceinline__ void store_nothing(const Layout<T, N, F>& lay, T* grad, float* loss) {
+  if (loss && lay.tid == 0) *loss = 0.0f;
+  if (grad) {
+#pragma unroll
+    for (int i = 0; i < Layout<T, N, F>::kVecs; ++i)
+      if (i < lay.vecs) *reinterpret_cast<Bytes16*>(grad + lay.vec_label(i)) = Bytes16{};
+#pragma unroll
+    for (int j = 0; j < Layout<T, N, F>::kVec; ++j) {
+      if (j >= lay.left) break;
+      if (lay.left_label(j) < lay.W) grad[lay.left_label(j)] = T{};
+    }
+  }
+}
+
+__device__ __forceinline__ float reference(float m) { return m > kNegInf ? m : 0.0f; }
+
 template <typename T, int N, int F, int PHASE>
-__global__ void __launch_bounds__(kThreads) distill_kernel(const DistillParams p, const DistillPlan plan, SpanSums* sums) {
+__global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(F > 16 ? 4 : 8)))
+distill_kernel(const DistillParams p, const DistillPlan plan, SpanSums* sums) {
   using L = Layout<T, N, F>;
   constexpr int V = L::kVec, kTeams = kThreads / N;
-  extern __shared__ __align__(16) float tables[];
-  __shared__ float red_all[kTeams][2][N / 64];
-  const int tid = threadIdx.x % N, team = threadIdx.x / N, lane = threadIdx.x & 63;
+  extern __shared__ __align__(16) char stages[];
+  __shared__ float red_all[kTeams][4][N / 64];
+  const int tid = threadIdx.x % N, team = team_of<N>(), lane = threadIdx.x & 63;
   const bool first_wave = tid < 64;
   Team<N> tm(red_all[team]);
-  const int64_t row = static_cast<int64_t>(blockIdx.x) * kTeams + team;
-  if (row >= static_cast<int64_t>(p.in.B) * p.in.T) return;  // (a wave's row: no barrier is passed below)
-  const int b = static_cast<int>(row / p.in.T), t = static_cast<int>(row % p.in.T);
+  const uint32_t at = blockIdx.x * kTeams + team, T_ = p.in.T;
+  if (at >= p.in.B * T_) return;  // (a wave's row: no barrier is passed below)
+  const int b = at / T_, t = at % T_;
+  const int64_t row = at;
   const int span = PHASE == kOneLaunch ? 0 : blockIdx.y, c0 = PHASE == kOneLaunch ? 0 : span * plan.span;
   const L lay(PHASE == kOneLaunch ? p.in.W : min(p.in.W - c0, plan.span), tid);
-  const T* in = static_cast<const T*>(p.in.data) + b * p.in.stride_b + t * p.in.stride_t + c0;
   T* grad = p.grad && PHASE != kSpanSums ? static_cast<T*>(p.grad) + b * p.grad_stride_b + t * p.grad_stride_t + c0 : nullptr;
-  const bool writes_loss = p.loss && PHASE != kSpanSums && span == 0 && first_wave;
-  const auto nothing = [&]() {
-    if (writes_loss && lane == 0) p.loss[row] = 0.0f;
-    if (grad) {
-#pragma unroll
-      for (int i = 0; i < L::kVecs; ++i)
-        if (i < lay.vecs) *reinterpret_cast<Bytes16*>(grad + lay.vec_label(i)) = Bytes16{};
-#pragma unroll
-      for (int j = 0; j < V; ++j)
-        if (j < lay.left && lay.left_label(j) < lay.W) grad[lay.left_label(j)] = T{};
-    }
-  };
-  if (t >= length_of(p.in, b)) return nothing();
+  float* loss = p.loss && PHASE != kSpanSums && span == 0 ? p.loss + row : nullptr;
+  if (t >= length_of(p.in, b)) return store_nothing(lay, grad, loss);
+  RawRow<T, N, F> x(lay, static_cast<const T*>(p.in.data) + b * p.in.stride_b + t * p.in.stride_t + c0);
+  List list(p, row, c0, lay.W);
+  if (!list.any) return store_nothing(lay, grad, loss);
 
-  // the teacher's list, two entries a lane, by every wave alike
-  float u[2], prob[2], log_prob[2];
-  int id[2];
+  // the list out of the row
+  T* stage = reinterpret_cast<T*>(stages) + team * ((lay.W + V - 1) / V * V);
 #pragma unroll
-  for (int e = 0; e < 2; ++e) {
-    const int i = lane + 64 * e;
-    u[e] = kNegInf;
-    id[e] = -1;
-    if (i < p.k) {
-      const int at = p.ids[row * p.k + i];
-      const float v = clean(p.values[row * p.k + i]);
-      if (at >= 0 && at < p.in.W && v > kNegInf) {
-        id[e] = at - c0;  // within this span or not
-        u[e] = fminf(v * p.scale, kLargest);
-      }
-    }
-    if (id[e] >= lay.W) id[e] = -1;
+  for (int i = 0; i < L::kVecs; ++i)
+    if (i < lay.vecs) *reinterpret_cast<uint4*>(stage + lay.vec_label(i)) = __builtin_bit_cast(uint4, x.raw[i]);
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    if (j >= lay.left) break;
+    if (lay.left_label(j) < lay.W) stage[lay.left_label(j)] = x.one[j];
   }
-  const float rest = p.tail ? clean(p.tail[row]) : kNegInf;
-  const bool with_rest = rest > kNegInf;
-  RawRow<T, N, F> x(lay, in);
-  float at_id[2];  // the student's scores of the listed labels
-#pragma unroll
-  for (int e = 0; e < 2; ++e) at_id[e] = id[e] >= 0 && first_wave ? to_float(in[id[e]]) : 0.0f;
-
-  const float mt = fmaxf(wave_max(fmaxf(u[0], u[1])), rest);
-  if (!(mt > kNegInf)) return nothing();
-#pragma unroll
-  for (int e = 0; e < 2; ++e) prob[e] = exp2_((u[e] - mt) * kLog2e);
-  const float rest_e = exp2_((rest - mt) * kLog2e), Z = wave_sum(prob[0] + prob[1]) + rest_e;
-  const float log_z = logf(Z), rest_p = rest_e / Z;
-#pragma unroll
-  for (int e = 0; e < 2; ++e) {
-    prob[e] /= Z;
-    log_prob[e] = (u[e] - mt) - log_z;
-  }
-
-  // their table
-  const int places = (lay.W + 3) / 4 * 4;
-  float* table = tables + team * places;
-  for (int i = tid; i < places / 4; i += N) reinterpret_cast<float4*>(table)[i] = float4{0.0f, 0.0f, 0.0f, 0.0f};
   tm.sync();
   if (first_wave) {
+    using Mark = decltype(bits_of(T{}));
+    volatile Mark* mark = reinterpret_cast<volatile Mark*>(stage);
     bool again = false;
-#pragma unroll
-    for (int e = 0; e < 2; ++e)
-      if (id[e] >= 0) again |= atomicExch(&table[id[e]], fmaxf(prob[e], kListed)) != 0.0f;
-    if (__ballot(again)) {
-      // labels listed more than once: their first entry takes the sum, in the list's order
-      float sum[2] = {0.0f, 0.0f};
-      bool first[2] = {true, true};
-      for (int i = 0; i < p.k; ++i) {
-        const int other = i < 64 ? __shfl(id[0], i) : __shfl(id[1], i - 64);
-        const float more = i < 64 ? __shfl(prob[0], i) : __shfl(prob[1], i - 64);
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-          if (id[e] >= 0 && other == id[e]) {
-            sum[e] += more;
-            if (i < lane + 64 * e) first[e] = false;
-          }
-      }
-#pragma unroll
-      for (int e = 0; e < 2; ++e)
-        if (id[e] >= 0) {
-          if (first[e]) table[id[e]] = fmaxf(sum[e], kListed);
-          prob[e] = first[e] ? sum[e] : 0.0f;
-          log_prob[e] = logf(sum[e]);
-        }
-    }
+    list.each([&](int d) {
+      if (list.id[d] >= 0) list.score[d] = to_float(from_bits(mark[list.id[d]], T{}));
+    });
+    list.each([&](int d) {
+      if (list.id[d] >= 0) mark[list.id[d]] = static_cast<Mark>(lane + 64 * d);
+    });
+    tm.wave_order();
+    list.each([&](int d) {
+      if (list.id[d] >= 0) again |= mark[list.id[d]] != static_cast<Mark>(lane + 64 * d);
+    });
+    if (__ballot(again)) list.sum_equal_labels(p.k);
+    tm.wave_order();
+    T none;
+    from_float(kNegInf, &none);
+    list.each([&](int d) {
+      if (list.id[d] >= 0) mark[list.id[d]] = bits_of(none);
+    });
   }
   tm.sync();
+#pragma unroll
+  for (int i = 0; i < L::kVecs; ++i)
+    if (i < lay.vecs) x.raw[i] = __builtin_bit_cast(Bytes16, *reinterpret_cast<const uint4*>(stage + lay.vec_label(i)));
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    if (j >= lay.left) break;
+    if (lay.left_label(j) < lay.W) x.one[j] = stage[lay.left_label(j)];
+  }
 
-  // m, S, and R relative to r
   const float c = p.scale * kLog2e;
-  float m, S, r, R;
-  // f(values, table entries, first label) of each vector, then of each label left
-  const auto with_table = [&](auto vec, auto one) {
-#pragma unroll
-    for (int i = 0; i < L::kVecs; ++i)
-      if (i < lay.vecs) {
-        float v[V];
-        unpack(x.raw[i], v, T());
-        float q[V];
-#pragma unroll
-        for (int d = 0; d < V / 4; ++d) {
-          const float4 f = *reinterpret_cast<const float4*>(&table[lay.vec_label(i) + 4 * d]);
-          q[4 * d] = f.x;
-          q[4 * d + 1] = f.y;
-          q[4 * d + 2] = f.z;
-          q[4 * d + 3] = f.w;
-        }
-        vec(v, q, lay.vec_label(i));
-      }
-#pragma unroll
-    for (int j = 0; j < V; ++j)
-      if (j < lay.left && lay.left_label(j) < lay.W) one(to_float(x.one[j]), table[lay.left_label(j)], lay.left_label(j));
-  };
-  const auto each_with_table = [&](auto f) {
-    with_table(
-        [&](const float* v, const float* q, int) {
-#pragma unroll
-          for (int e = 0; e < V; ++e) f(v[e], q[e]);
-        },
-        [&](float v, float q, int) { f(v, q); });
-  };
-  if (PHASE != kSpanGrads) {
-    m = kNegInf;
-    x.each(lay, [&](float v, int) { m = fmaxf(m, v); });
-    m = tm.max(m);
-    if (m == kNegInf) {
-      // nothing but -inf, or NaN among it, which is to be seen
-      float nan = 0.0f;
-      x.each(lay, [&](float v, int) { nan = v != v ? 1.0f : nan; });
-      if (tm.max(nan) != 0.0f) m = 0.0f;
-      else if (PHASE == kOneLaunch) return nothing();
-    }
-    const float m0 = m == kNegInf ? 0.0f : m;
-    S = R = 0.0f;
-    r = m;
-    x.forget();
-    if (with_rest) {
-      each_with_table([&](float v, float q) {
-        const float e = exp2_((v - m0) * c);
-        S += e;
-        R += q != 0.0f ? 0.0f : e;
-      });
-      S = tm.sum(S);
-      R = tm.sum(R);
-      if (R < kSmallRest) {
-        x.forget();
-        r = kNegInf;
-        each_with_table([&](float v, float q) { r = fmaxf(r, q != 0.0f ? kNegInf : v); });
-        r = tm.max(r);
-        R = 0.0f;
-        if (r > kNegInf) {
-          each_with_table([&](float v, float q) { R += q != 0.0f ? 0.0f : exp2_((v - r) * c); });
-          R = tm.sum(R);
-        }
-      }
-    } else {
-      x.each(lay, [&](float v, int) { S += exp2_((v - m0) * c); });
-      S = tm.sum(S);
-    }
-  }
-  if (PHASE == kSpanSums) {
-    float terms = 0.0f, listed = 0.0f;
-    if (first_wave) {
-      const float m0 = m == kNegInf ? 0.0f : m;
-#pragma unroll
-      for (int e = 0; e < 2; ++e)
-        if (id[e] >= 0 && prob[e] > 0.0f) {
-          terms += prob[e] * (log_prob[e] - (at_id[e] - m0) * p.scale);
-          listed += prob[e];
-        }
-      terms = wave_sum(terms);
-      listed = wave_sum(listed);
-      if (lane == 0) sums[row * plan.spans + span] = {m, S, r, R, terms, listed};
-    }
-    return;
-  }
-  float term = 0.0f;  // of the loss, but for the rest's
+  float m, r, R, listed_sum, terms, listed;
   if (PHASE == kSpanGrads) {
     const SpanSums* all = sums + row * plan.spans;
     m = r = kNegInf;
@@ -258,61 +260,85 @@ __global__ void __launch_bounds__(kThreads) distill_kernel(const DistillParams p
     }
     m = wave_max(m);
     r = wave_max(r);
-    if (m == kNegInf) return nothing();
-    S = R = 0.0f;
-    float listed = 0.0f;
+    R = listed_sum = terms = listed = 0.0f;
     for (int i = lane; i < plan.spans; i += 64) {
       const SpanSums a = all[i];
-      if (a.m != kNegInf) S += a.S * exp2_((a.m - m) * c);
-      if (a.R > 0.0f) R += a.R * exp2_((a.r - r) * c);
-      if (a.listed > 0.0f) term += a.terms + a.listed * ((m - (a.m == kNegInf ? 0.0f : a.m)) * p.scale);
+      R += a.R > 0.0f ? a.R * exp2_((a.r - r) * c) : a.R;
+      if (a.listed_sum != 0.0f) listed_sum += a.listed_sum * exp2_((reference(a.m) - reference(m)) * c);
+      if (a.listed > 0.0f) terms += a.terms + a.listed * ((reference(m) - reference(a.m)) * p.scale);
       listed += a.listed;
     }
-    S = wave_sum(S);
     R = wave_sum(R);
-    const float beside = R * exp2_((r - m) * c);
-    if (beside >= kSmallRest) {
-      R = beside;
-      r = m;
-    }
-    term = wave_sum(term) + wave_sum(listed) * logf(S);
+    listed_sum = wave_sum(listed_sum);
   } else {
-    const float log_s = logf(S);
-#pragma unroll
-    for (int e = 0; e < 2; ++e)
-      if (id[e] >= 0 && prob[e] > 0.0f) term += prob[e] * (log_prob[e] - ((at_id[e] - m) * p.scale - log_s));
-    if (writes_loss) term = wave_sum(term);
+    r = x.largest(lay);
+    m = first_wave ? fmaxf(r, list.largest()) : r;
+    tm.join2(r, m, Max());
+    R = 0.0f;
   }
-  if (writes_loss && lane == 0) {
-    if (rest_p > 0.0f) {
-      const float log_q = R > 0.0f ? (r - m) * p.scale + logf(R) - logf(S) : S != S ? S : kNegInf;
-      term += rest_p * ((rest - mt) - log_z - log_q);
+  float e[F + V];
+  if (PHASE != kSpanGrads || grad) {
+    const float ref = reference(r);
+    lay.each([&](int i, int) {
+      e[i] = exp2_((x.value(i) - ref) * c);
+      if (PHASE != kSpanGrads) R += e[i];
+    });
+  }
+  if (PHASE != kSpanGrads) {
+    listed_sum = first_wave ? list.sum(reference(m), c) : 0.0f;
+    tm.join2(R, listed_sum, Sum());
+    terms = list.terms(reference(m), p.scale);
+    listed = list.listed();
+  }
+  if (PHASE == kSpanSums) {
+    if (first_wave) {
+      terms = wave_sum(terms);
+      listed = wave_sum(listed);
+      if (tid == 0) sums[row * plan.spans + span] = {m, listed_sum, r, R, terms, listed};
     }
-    p.loss[row] = term;
+    return;
+  }
+  const RowSums of(reference(m), r, R, listed_sum, c);
+  if (of.S == 0.0f) return store_nothing(lay, grad, loss);  // a row of -inf
+  if (loss && first_wave) {
+    // (of spans, each lane has sums of other spans)
+    const float l = wave_sum(terms + (listed > 0.0f ? listed * log_(of.S) : 0.0f)) + of.rest_loss(list, p.scale);
+    if (tid == 0) *loss = l;
   }
   if (!grad) return;
 
-  const float w = (p.weights ? p.weights[b * p.weight_stride_b + t * p.weight_stride_t] : p.weight) * p.scale;
-  const float a = w / S, per_rest = R > 0.0f ? w * rest_p / R : 0.0f;
-  x.forget();
-  const auto store = [&](auto g) {
-    with_table(
-        [&](const float* v, const float* q, int label) {
-          float o[V];
+  // the gradient, and the list back into it
+  const float w = row_weight(p, b, t), rest = of.rest_factor(w, c, list);
 #pragma unroll
-          for (int e = 0; e < V; ++e) o[e] = g(v[e], q[e]);
-          store_vec(grad + label, o);
-        },
-        [&](float v, float q, int label) { from_float(g(v, q), &grad[label]); });
-  };
-  if (r == m || !(per_rest != 0.0f)) {
-    const float a_rest = a - per_rest;
-    store([&](float v, float q) { return exp2_((v - m) * c) * (q != 0.0f ? a : a_rest) - q * w; });
-  } else {
-    store([&](float v, float q) {
-      const float e = exp2_((v - m) * c) * a;
-      return q != 0.0f ? e - q * w : e - exp2_((v - r) * c) * per_rest;
+  for (int i = 0; i < L::kVecs; ++i)
+    if (i < lay.vecs) {
+      float o[V];
+#pragma unroll
+      for (int d = 0; d < V; ++d) o[d] = e[i * V + d] * rest;
+      *reinterpret_cast<uint4*>(stage + lay.vec_label(i)) = pack(o, T{});
+    }
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    if (j >= lay.left) break;
+    if (lay.left_label(j) < lay.W) from_float(e[F + j] * rest, &stage[lay.left_label(j)]);
+  }
+  tm.sync();
+  if (first_wave) {
+    const float a = of.listed_factor(w);
+    list.each([&](int d) {
+      if (list.id[d] >= 0) from_float(exp2_((list.score[d] - of.m) * c) * a - list.prob[d] * w, &stage[list.id[d]]);
     });
+  }
+  tm.sync();
+#pragma unroll
+  for (int i = 0; i < L::kVecs; ++i)
+    if (i < lay.vecs)
+      *reinterpret_cast<Bytes16*>(grad + lay.vec_label(i)) =
+          __builtin_bit_cast(Bytes16, *reinterpret_cast<const uint4*>(stage + lay.vec_label(i)));
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    if (j >= lay.left) break;
+    if (lay.left_label(j) < lay.W) grad[lay.left_label(j)] = stage[lay.left_label(j)];
   }
 }
 
@@ -329,7 +355,7 @@ template <typename T, int N, int F>
 static void run_distill(const DistillParams& p, const DistillPlan& q, SpanSums* sums, hipStream_t stream) {
   constexpr int teams = kThreads / N;
   const int64_t rows = static_cast<int64_t>(p.in.B) * p.in.T;
-  const size_t lds = sizeof(float) * teams * ((std::min(q.span, p.in.W) + 3) / 4 * 4);
+  const size_t lds = static_cast<size_t>(teams) * ((std::min(q.span, p.in.W) * sizeof(T) + 15) / 16 * 16);
   const uint32_t groups = static_cast<uint32_t>((rows + teams - 1) / teams);
   if constexpr (N > 64) {
     if (q.spans > 1) {

@@ -32,8 +32,8 @@ __global__ void __launch_bounds__(kThreads) process_kernel(const ProcessParams p
   using L = Layout<T, N, F>;
   constexpr int V = L::kVec;
   extern __shared__ uint32_t count[];
-  __shared__ float red[2][N / 64 < 1 ? 1 : N / 64];
-  const int tid = threadIdx.x % N, team = threadIdx.x / N, teams = kThreads / N;
+  __shared__ float red[4][N / 64];
+  const int tid = threadIdx.x % N, team = team_of<N>(), teams = kThreads / N;
   const int span = blockIdx.y, b = blockIdx.x / plan.groups;
   const int t0 = (blockIdx.x % plan.groups) * plan.frames;
   const int T1 = min(length_of(p.in, b), t0 + plan.frames);
@@ -110,8 +110,9 @@ __global__ void __launch_bounds__(kThreads) process_kernel(const ProcessParams p
         for (int e = 0; e < V; ++e) m = fmaxf(m, y[e]);
       }
 #pragma unroll
-    for (int j = 0; j < V; ++j)
-      if (j < lay.left && lay.left_label(j) < lay.W) {
+    for (int j = 0; j < V; ++j) {
+      if (j >= lay.left) break;
+      if (lay.left_label(j) < lay.W) {
         const int c = lay.left_label(j);
         float v = clean(x[F + j]);
         if (H) v = seen(v, count[c]);
@@ -120,6 +121,7 @@ __global__ void __launch_bounds__(kThreads) process_kernel(const ProcessParams p
         x[F + j] = v;
         m = fmaxf(m, v);
       }
+    }
 
     float total = 0.0f;
     if (PHASE == kStats || (PHASE == kWhole && p.normalize)) {
@@ -149,8 +151,10 @@ __global__ void __launch_bounds__(kThreads) process_kernel(const ProcessParams p
         store_floats<V>(out + lay.vec_label(i), y);
       }
 #pragma unroll
-    for (int j = 0; j < V; ++j)
-      if (j < lay.left && lay.left_label(j) < lay.W) out[lay.left_label(j)] = x[F + j] - total;
+    for (int j = 0; j < V; ++j) {
+      if (j >= lay.left) break;
+      if (lay.left_label(j) < lay.W) out[lay.left_label(j)] = x[F + j] - total;
+    }
   }
 }
 

@@ -16,6 +16,7 @@ constexpr float kLargest = 3.402823466e38f;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
+
 struct F16 { uint16_t u; };
 struct BF16 { uint16_t u; };
 
@@ -30,7 +31,25 @@ __device__ __forceinline__ void from_float(float v, BF16* o) { o->u = __builtin_
 // NaN counts as -inf, +inf as the largest number
 __device__ __forceinline__ float clean(float v) { return fminf(fmaxf(v, kNegInf), kLargest); }
 
+__device__ __forceinline__ uint32_t bits_of(float v) { return __float_as_uint(v); }
+__device__ __forceinline__ uint16_t bits_of(F16 v) { return v.u; }
+__device__ __forceinline__ uint16_t bits_of(BF16 v) { return v.u; }
+__device__ __forceinline__ float from_bits(uint32_t u, float) { return __uint_as_float(u); }
+template <typename T>
+__device__ __forceinline__ T from_bits(uint16_t u, T) { return T{u}; }
+
+// The hardware's 2^x, logarithm and reciprocal: one step of fp32 each, for the
+// numbers they are asked for here (sums from 1 on, exponents from 0 down).
 __device__ __forceinline__ float exp2_(float v) { return __builtin_amdgcn_exp2f(v); }
+__device__ __forceinline__ float log_(float v) { return __builtin_amdgcn_logf(v) * kLn2; }
+__device__ __forceinline__ float rcp_(float v) { return __builtin_amdgcn_rcpf(v); }
+
+// The larger of three (of two); where one is NaN, any of them.
+__device__ __forceinline__ float max3_any(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
 
 // 16 bytes at any address: rows of an odd number of labels start anywhere.
 struct __attribute__((packed, aligned(2))) Bytes16 { uint32_t w[4]; };
@@ -57,6 +76,31 @@ __device__ __forceinline__ void unpack(const Bytes16& b, float* o, BF16) {
     o[2 * i] = __uint_as_float(b.w[i] << 16);
     o[2 * i + 1] = __uint_as_float(b.w[i] & 0xFFFF0000u);
   }
+}
+
+// 16 bytes of values, each rounded once
+__device__ __forceinline__ uint4 pack(const float* v, float) {
+  return {__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+}
+template <typename T>
+__device__ __forceinline__ uint4 pack(const float* v, T) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    T lo, hi;
+    from_float(v[2 * i], &lo);
+    from_float(v[2 * i + 1], &hi);
+    w[i] = static_cast<uint32_t>(lo.u) | (static_cast<uint32_t>(hi.u) << 16);
+  }
+  return {w[0], w[1], w[2], w[3]};
+}
+
+// Which of a workgroup's rows a thread is at: the same for its whole wave,
+// which keeps the row's addresses in scalar registers.
+template <int N>
+__device__ __forceinline__ int team_of() {
+  if constexpr (N >= kThreads) return 0;
+  else return __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / N);
 }
 
 // ---- over a wave: every lane gets the result, and the same bits of it ----
@@ -88,9 +132,30 @@ __device__ __forceinline__ float wave_sum(float v) { return wave_join(v, Sum());
 // is enough.
 template <int N>
 struct Team {
-  float (*lds)[N / 64];
+  float (*lds)[N / 64];  // [4]
   int turn = 0;
   __device__ __forceinline__ explicit Team(float (*l)[N / 64]) : lds(l) {}
+  // two values by the same operation
+  template <typename Op>
+  __device__ __forceinline__ void join2(float& a, float& b, Op op) {
+    a = wave_join(a, op);
+    b = wave_join(b, op);
+    if constexpr (N > 64) {
+      if ((threadIdx.x & 63) == 0) {
+        lds[turn][threadIdx.x >> 6] = a;
+        lds[turn + 1][threadIdx.x >> 6] = b;
+      }
+      __syncthreads();
+      a = lds[turn][0];
+      b = lds[turn + 1][0];
+#pragma unroll
+      for (int i = 1; i < N / 64; ++i) {
+        a = op(a, lds[turn][i]);
+        b = op(b, lds[turn + 1][i]);
+      }
+      turn ^= 2;
+    }
+  }
   template <typename Op>
   __device__ __forceinline__ float join(float v, Op op) {
     v = wave_join(v, op);
@@ -100,16 +165,20 @@ struct Team {
       v = lds[turn][0];
 #pragma unroll
       for (int i = 1; i < N / 64; ++i) v = op(v, lds[turn][i]);
-      turn ^= 1;
+      turn ^= 2;
     }
     return v;
   }
   __device__ __forceinline__ float max(float v) { return join(v, Max()); }
   __device__ __forceinline__ float sum(float v) { return join(v, Sum()); }
+  // between what one thread of the row writes to LDS and another reads
   __device__ __forceinline__ void sync() {
     if constexpr (N > 64) __syncthreads();
-    else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    else wave_order();
   }
+  // the same within a wave, whose LDS accesses complete in order: nothing is
+  // to be reordered by the compiler
+  __device__ __forceinline__ void wave_order() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
 };
 
 // The labels of a row (or of a span of it), spread over N threads: first whole
@@ -137,8 +206,10 @@ struct Layout {
         for (int e = 0; e < kVec; ++e) f(i * kVec + e, vec_label(i) + e);
       }
 #pragma unroll
-    for (int j = 0; j < kVec; ++j)
-      if (j < left && left_label(j) < W) f(F + j, left_label(j));
+    for (int j = 0; j < kVec; ++j) {
+      if (j >= left) break;
+      if (left_label(j) < W) f(F + j, left_label(j));
+    }
   }
   // x[0 .. F+kVec): the row's scores as fp32; `fill` where there is no label
   __device__ __forceinline__ void load(const T* row, float* x, float fill) const {
@@ -148,8 +219,10 @@ struct Layout {
     for (int i = 0; i < kVecs; ++i)
       if (i < vecs) raw[i] = *reinterpret_cast<const Bytes16*>(row + vec_label(i));
 #pragma unroll
-    for (int j = 0; j < kVec; ++j)
-      if (j < left && left_label(j) < W) one[j] = row[left_label(j)];
+    for (int j = 0; j < kVec; ++j) {
+      if (j >= left) break;
+      if (left_label(j) < W) one[j] = row[left_label(j)];
+    }
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
       if (i < vecs) {
@@ -175,8 +248,10 @@ struct RawRow {
     for (int i = 0; i < L::kVecs; ++i)
       if (i < lay.vecs) raw[i] = *reinterpret_cast<const Bytes16*>(row + lay.vec_label(i));
 #pragma unroll
-    for (int j = 0; j < L::kVec; ++j)
-      if (j < lay.left && lay.left_label(j) < lay.W) one[j] = row[lay.left_label(j)];
+    for (int j = 0; j < L::kVec; ++j) {
+      if (j >= lay.left) break;
+      if (lay.left_label(j) < lay.W) one[j] = row[lay.left_label(j)];
+    }
   }
   // f(value, label, there) for the labels of this thread, by all threads alike:
   // `there` is false behind the last label
@@ -199,6 +274,31 @@ struct RawRow {
     every(lay, [&](float v, int label, bool there) {
       if (there) f(v, label);
     });
+  }
+  // the largest value, where no value is NaN
+  __device__ __forceinline__ float largest(const L& lay) const {
+    float m = kNegInf;
+#pragma unroll
+    for (int i = 0; i < L::kVecs; ++i)
+      if (i < lay.vecs) {
+        float v[L::kVec];
+        unpack(raw[i], v, T());
+#pragma unroll
+        for (int e = 0; e < L::kVec; e += 2) m = max3_any(m, v[e], v[e + 1]);
+      }
+#pragma unroll
+    for (int j = 0; j < L::kVec; ++j) {
+      if (j >= lay.left) break;
+      if (lay.left_label(j) < lay.W) m = fmaxf(m, to_float(one[j]));
+    }
+    return m;
+  }
+  // the i-th value as Layout::each counts them, i known when unrolled
+  __device__ __forceinline__ float value(int i) const {
+    if (i >= F) return to_float(one[i - F]);
+    float v[L::kVec];
+    unpack(raw[i / L::kVec], v, T());
+    return v[i % L::kVec];
   }
   // What follows unpacks the row anew, instead of keeping unpacked (or
   // otherwise derived) values of all labels in registers from before.

@@ -63,17 +63,18 @@ __global__ void __launch_bounds__(N > kThreads ? N : kThreads) top_kernel(const 
   constexpr int kTeams = N > kThreads ? 1 : kThreads / N;
   constexpr int kMaxima = N == 64 ? 64 : 256;  // groups whose maxima give the bound
   constexpr int kRoom = 4 * N, kOwn = kRoom / N;
-  __shared__ float red_all[kTeams][2][N / 64];
+  __shared__ float red_all[kTeams][4][N / 64];
   __shared__ __align__(16) uint64_t room_all[kTeams][kRoom + 2];
   __shared__ uint32_t maxima[N == 64 ? 1 : kMaxima];
   __shared__ int found_lds;
   __shared__ uint64_t last_all[kTeams];
-  const int tid = threadIdx.x % N, team = threadIdx.x / N, lane = threadIdx.x & 63;
+  const int tid = threadIdx.x % N, team = team_of<N>(), lane = threadIdx.x & 63;
   Team<N> tm(red_all[team]);
   uint64_t* room = room_all[team];
-  const int64_t row = static_cast<int64_t>(blockIdx.x) * kTeams + team;
-  if (row >= static_cast<int64_t>(p.in.B) * p.in.T) return;  // (a wave's row: no barrier is passed below)
-  const int b = static_cast<int>(row / p.in.T), t = static_cast<int>(row % p.in.T);
+  const uint32_t at = blockIdx.x * kTeams + team, T_ = p.in.T;
+  if (at >= p.in.B * T_) return;  // (a wave's row: no barrier is passed below)
+  const int b = at / T_, t = at % T_;
+  const int64_t row = at;
   if (t >= length_of(p.in, b)) {
     if (!PART) {
       for (int i = tid; i < p.k; i += N) {
@@ -247,10 +248,11 @@ __global__ void __launch_bounds__(N > kThreads ? N : kThreads) top_kernel(const 
 // its own list plus the larger keys of the others, which are in order.
 __global__ void __launch_bounds__(kThreads) join_top_kernel(const TopParams p, const TopPlan plan, const void* ws) {
   extern __shared__ uint64_t lists[];  // [spans][k]
-  __shared__ float red[2][kThreads / 64];
+  __shared__ float red[4][kThreads / 64];
   const int tid = threadIdx.x, k = p.k, n = plan.spans * k;
   const int64_t row = blockIdx.x;
-  const int b = static_cast<int>(row / p.in.T), t = static_cast<int>(row % p.in.T);
+  const uint32_t T_ = p.in.T;
+  const int b = blockIdx.x / T_, t = blockIdx.x % T_;
   if (t >= length_of(p.in, b)) {
     for (int i = tid; i < k; i += kThreads) {
       p.values[row * k + i] = kNegInf;

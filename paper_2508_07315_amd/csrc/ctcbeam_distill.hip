@@ -32,7 +32,7 @@ enum DistillPhase { kOneLaunch = 0, kSpanSums = 1, kSpanGrads = 2 };
 
 struct DistillPlan {
   int n, f;   // threads of a row (of a span), labels of a thread
-  int spans;  // per row
+  int spans;  // per row; 0: a workgroup holds the row in packed registers
   int span;   // labels of a span (the last one may hold fewer)
 };
 
@@ -50,6 +50,7 @@ struct List {
   float rest_p, log_rest_p;
   bool any, two;  // more than 64 entries: the lanes' second ones
 
+  List() = default;
   __device__ __forceinline__ List(const DistillParams& p, int64_t row, int c0, int W) {
     const int lane = threadIdx.x & 63;
     two = p.k > 64;
@@ -156,8 +157,8 @@ struct RowSums {
     return list.rest_p * (list.log_rest_p - log_q);
   }
   __device__ __forceinline__ float listed_factor(float w) const { return w * rcp_(S); }
-  __device__ __forceinline__ float rest_factor(float w, float c, const List& list) const {
-    return (r > kNegInf ? exp2_((r - m) * c) : 0.0f) * (w * rcp_(S)) - (R > 0.0f ? w * list.rest_p * rcp_(R) : 0.0f);
+  __device__ __forceinline__ float rest_factor(float w, float c, float rest_p) const {
+    return (r > kNegInf ? exp2_((r - m) * c) : 0.0f) * (w * rcp_(S)) - (R > 0.0f ? w * rest_p * rcp_(R) : 0.0f);
   }
 };
 
@@ -308,7 +309,7 @@ distill_kernel(const DistillParams p, const DistillPlan plan, SpanSums* sums) {
   if (!grad) return;
 
   // the gradient, and the list back into it
-  const float w = row_weight(p, b, t), rest = of.rest_factor(w, c, list);
+  const float w = row_weight(p, b, t), rest = of.rest_factor(w, c, list.rest_p);
 #pragma unroll
   for (int i = 0; i < L::kVecs; ++i)
     if (i < lay.vecs) {
@@ -342,10 +343,170 @@ distill_kernel(const DistillParams p, const DistillPlan plan, SpanSums* sums) {
   }
 }
 
-static DistillPlan plan_distill(int B, int T, int W) {
+// Rows that a workgroup holds in packed registers.  A bit per
+// label in LDS says which are listed; few vectors of a wave hold one, and only
+// those look their gradient up, in a table of four places an entry, each
+// label at the first free one from its own on.  One workgroup fills a compute unit, so reading,
+// computing and writing overlap between units, not within one.
+constexpr int kPlaces = 4 * kMaxTop;
+
+template <typename T, int N, int VECS>
+__global__ void __launch_bounds__(N) distill_wide_kernel(const DistillParams p) {
+  using L = Layout<T, N, VECS * Packed<T>::kVec>;
+  constexpr int V = L::kVec, kWords = N * (VECS + 1) * V / 32;
+  __shared__ __align__(16) uint32_t bits[kWords];
+  __shared__ float red[4][N / 64];
+  __shared__ int place_label[kPlaces];
+  __shared__ float place_grad[kPlaces];
+  __shared__ int any;
+  __shared__ float rest_p;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const bool first_wave = tid < 64;
+  Team<N> tm(red);
+  const uint32_t row = blockIdx.x, T_ = p.in.T;
+  const int b = row / T_, t = row % T_;
+  const L lay(p.in.W, tid);
+  const T* in = static_cast<const T*>(p.in.data) + b * p.in.stride_b + t * p.in.stride_t;
+  T* grad = p.grad ? static_cast<T*>(p.grad) + b * p.grad_stride_b + t * p.grad_stride_t : nullptr;
+  float* loss = p.loss ? p.loss + row : nullptr;
+  if (t >= length_of(p.in, b)) return store_nothing(lay, grad, loss);
+  RawRow<T, N, L::kVecs * V> x(lay, in);
+  List list;
+  int place[2];
+  for (int i = tid; i < (lay.W + 31) / 32; i += N) bits[i] = 0;
+  for (int i = tid; i < kPlaces; i += N) place_label[i] = -1;
+  if (first_wave) {
+    list = List(p, row, 0, lay.W);
+    list.each([&](int d) {
+      if (list.id[d] >= 0) list.score[d] = to_float(in[list.id[d]]);
+    });
+    if (lane == 0) {
+      any = list.any;
+      rest_p = list.rest_p;
+    }
+  }
+  __syncthreads();
+  if (!any) return store_nothing(lay, grad, loss);
+  if (first_wave) {
+    bool again = false;
+    list.each([&](int d) {
+      const uint32_t bit = 1u << (list.id[d] & 31);
+      if (list.id[d] >= 0) again |= (atomicOr(&bits[list.id[d] >> 5], bit) & bit) != 0;
+    });
+    if (__ballot(again)) list.sum_equal_labels(p.k);
+    list.each([&](int d) {
+      if (list.id[d] < 0) return;
+      int at = list.id[d] % kPlaces;  // (at most kMaxTop labels: there is a free place)
+      while (atomicCAS(&place_label[at], -1, list.id[d]) != -1) at = (at + 1) % kPlaces;
+      place[d] = at;
+    });
+  }
+  __syncthreads();
+
+  // the list out of the row
+  const uint8_t* bytes = reinterpret_cast<const uint8_t*>(bits);
+  const auto flags_of = [&](int i) -> uint32_t {
+    const int at = i * N + tid;
+    if constexpr (V == 8) return bytes[at];
+    else return (bytes[at >> 1] >> (at & 1) * 4) & 15u;
+  };
+  const auto is_listed = [&](int label) { return ((bits[label >> 5] >> (label & 31)) & 1u) != 0; };
+  T none;
+  from_float(kNegInf, &none);
+  const uint32_t none_bits = bits_of(none);
+#pragma unroll
+  for (int i = 0; i < VECS; ++i)
+    if (i < lay.vecs) {
+      const uint32_t f = flags_of(i);
+      if (__ballot(f != 0)) {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          uint32_t& u = x.raw[i].w[w];
+          if constexpr (V == 8) {
+            if ((f >> (2 * w)) & 1u) u = (u & 0xFFFF0000u) | none_bits;
+            if ((f >> (2 * w)) & 2u) u = (u & 0x0000FFFFu) | (none_bits << 16);
+          } else {
+            if ((f >> w) & 1u) u = none_bits;
+          }
+        }
+      }
+    }
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    if (j >= lay.left) break;
+    if (lay.left_label(j) < lay.W && is_listed(lay.left_label(j))) x.one[j] = none;
+  }
+
+  const float c = p.scale * kLog2e;
+  float r = x.largest(lay), m = first_wave ? fmaxf(r, list.largest()) : r;
+  tm.join2(r, m, Max());
+  const float ref = reference(r);
+  float R = 0.0f, listed_sum = first_wave ? list.sum(reference(m), c) : 0.0f;
+  x.forget();
+  x.each(lay, [&](float v, int) { R += exp2_((v - ref) * c); });
+  tm.join2(R, listed_sum, Sum());
+  const RowSums of(reference(m), r, R, listed_sum, c);
+  if (of.S == 0.0f) return store_nothing(lay, grad, loss);  // a row of -inf
+  const float w = row_weight(p, b, t);
+  if (first_wave) {
+    if (loss) {
+      const float listed = list.listed();
+      const float l = wave_sum(list.terms(of.m, p.scale) + (listed > 0.0f ? listed * log_(of.S) : 0.0f));
+      if (lane == 0) *loss = l + of.rest_loss(list, p.scale);
+    }
+    const float a = of.listed_factor(w);
+    list.each([&](int d) {
+      const float g = exp2_((list.score[d] - of.m) * c) * a - list.prob[d] * w;
+      if (list.id[d] >= 0) place_grad[place[d]] = g;
+    });
+  }
+  if (!grad) return;
+  __syncthreads();
+  const float rest = of.rest_factor(w, c, rest_p);
+  x.forget();
+  const auto gradient_of = [&](int label) {
+    int at = label % kPlaces;  // (a listed label: it has a place)
+    while (place_label[at] != label) at = (at + 1) % kPlaces;
+    return place_grad[at];
+  };
+#pragma unroll
+  for (int i = 0; i < VECS; ++i)
+    if (i < lay.vecs) {
+      float v[V], o[V];
+      unpack(x.raw[i], v, T());
+#pragma unroll
+      for (int d = 0; d < V; ++d) o[d] = exp2_((v[d] - ref) * c) * rest;
+      uint32_t f = flags_of(i);
+      while (f) {
+        const int at = __ffs(f) - 1;
+        const float g = gradient_of(lay.vec_label(i) + at);
+#pragma unroll
+        for (int d = 0; d < V; ++d) o[d] = d == at ? g : o[d];
+        f &= f - 1;
+      }
+      *reinterpret_cast<Bytes16*>(grad + lay.vec_label(i)) = __builtin_bit_cast(Bytes16, pack(o, T{}));
+    }
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    if (j >= lay.left) break;
+    const int label = lay.left_label(j);
+    if (label < lay.W)
+      from_float(is_listed(label) ? gradient_of(label) : exp2_((to_float(x.one[j]) - ref) * c) * rest, &grad[label]);
+  }
+}
+
+// Rows from which on a workgroup for each fills the card.
+constexpr int64_t kManyRows = 128;
+
+static DistillPlan plan_distill(int type, int B, int T, int W) {
   const int64_t rows = static_cast<int64_t>(B) * T;
   if (W < 64 * 36 && rows >= 1024) return {64, W < 64 * 20 ? 16 : 32, 1, W};
   if (W < 256 * 36) return {256, W < 256 * 12 ? 8 : W < 256 * 20 ? 16 : 32, 1, W};
+  const int vec = type == kTypeF32 ? 4 : 8;
+  if (rows >= kManyRows && W < 1024 * 17 * vec) {
+    const int n = W < 256 * 17 * vec ? 256 : W < 512 * 17 * vec ? 512 : 1024;
+    return {n, (W < 256 * 9 * vec ? 8 : 16) * vec, 0, W};
+  }
   int span = 8192;
   while (span > 2048 && rows * ((W + span - 1) / span) < 512) span >>= 1;
   return {256, span / 256, (W + span - 1) / span, span};
@@ -369,8 +530,14 @@ static void run_distill(const DistillParams& p, const DistillPlan& q, SpanSums* 
 
 template <typename T>
 static hipError_t choose_distill(const DistillParams& p, SpanSums* sums, hipStream_t stream) {
-  const DistillPlan q = plan_distill(p.in.B, p.in.T, p.in.W);
-  if (q.n == 64) q.f == 16 ? run_distill<T, 64, 16>(p, q, sums, stream) : run_distill<T, 64, 32>(p, q, sums, stream);
+  const DistillPlan q = plan_distill(p.in.type, p.in.B, p.in.T, p.in.W);
+  const uint32_t rows = static_cast<uint32_t>(p.in.B) * p.in.T;
+  if (q.spans == 0) {
+    if (q.n == 1024) distill_wide_kernel<T, 1024, 16><<<rows, 1024, 0, stream>>>(p);
+    else if (q.n == 512) distill_wide_kernel<T, 512, 16><<<rows, 512, 0, stream>>>(p);
+    else if (q.f == 16 * Packed<T>::kVec) distill_wide_kernel<T, 256, 16><<<rows, 256, 0, stream>>>(p);
+    else distill_wide_kernel<T, 256, 8><<<rows, 256, 0, stream>>>(p);
+  } else if (q.n == 64) q.f == 16 ? run_distill<T, 64, 16>(p, q, sums, stream) : run_distill<T, 64, 32>(p, q, sums, stream);
   else if (q.f == 8) run_distill<T, 256, 8>(p, q, sums, stream);
   else if (q.f == 16) run_distill<T, 256, 16>(p, q, sums, stream);
   else run_distill<T, 256, 32>(p, q, sums, stream);
@@ -379,9 +546,14 @@ static hipError_t choose_distill(const DistillParams& p, SpanSums* sums, hipStre
 
 }  // namespace rows
 
+// (for either width of the scores, as the caller need not say it)
 size_t distill_workspace(int B, int T, int W) {
-  const rows::DistillPlan q = rows::plan_distill(B, T, W);
-  return q.spans == 1 ? 0 : static_cast<size_t>(B) * T * q.spans * sizeof(rows::SpanSums);
+  size_t most = 0;
+  for (int type : {kTypeF32, kTypeBF16}) {
+    const rows::DistillPlan q = rows::plan_distill(type, B, T, W);
+    if (q.spans > 1) most = std::max(most, static_cast<size_t>(B) * T * q.spans * sizeof(rows::SpanSums));
+  }
+  return most;
 }
 
 hipError_t launch_distill(const DistillParams& p, void* workspace, hipStream_t stream) {

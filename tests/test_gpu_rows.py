@@ -271,13 +271,15 @@ def test_distill_widths(i, W, kind):
 
 
 @pytest.mark.parametrize("B,T,W,k", [(1, 1, 262144, 128), (260, 1, 700, 4), (1, 300, 1025, 16), (30, 1, 20001, 50),
-                                     (300, 4, 33, 5), (2, 520, 1025, 128), (1030, 1, 2303, 16)])
+                                     (300, 4, 33, 5), (2, 520, 1025, 128), (1030, 1, 2303, 16),
+                                     (130, 1, 9216, 20), (2, 65, 40959, 128), (1, 140, 81921, 64), (128, 1, 139263, 9)])
 def test_distill_sizes(B, T, W, k):
     v, ids, tail = teacher(B, T, W, k, W)
     distill_case(scores(B, T, W, "bf16", W + 1), v, ids, tail, what=f"B={B} T={T} W={W}", kind="bf16")
 
 
-ODD_ROWS = [(50, 1), (1025, 1), (1025, 130), (2303, 130), (6000, 1), (90000, 1)]   # labels, times the 8 rows
+ODD_ROWS = [(50, 1), (1025, 1), (1025, 130), (2303, 130), (6000, 1), (90000, 1), (9300, 17),
+            (60001, 17)]                                   # labels, times the 8 rows
 
 
 @pytest.mark.parametrize("W,times", ODD_ROWS)
@@ -498,7 +500,7 @@ def test_graphs(B, T, W):
 
 
 def test_same_call_same_bits():
-    for B, T, W in ((3, 20, 1025), (2, 2, 20001), (1, 2, 200001)):
+    for B, T, W in ((3, 20, 1025), (2, 2, 20001), (1, 2, 200001), (130, 1, 20001)):
         x, ops = operators(B, T, W)
         for call, outs in ops:
             call()

@@ -549,7 +549,7 @@ class _ProcessOpts(ctypes.Structure):
                 ("reserved", ctypes.c_int * 3)]
 
 
-_TYPES = {"torch.float32": 0, "torch.float16": 1, "torch.bfloat16": 2}   # CTCBEAM_TYPE_*
+_TYPES = {}   # CTCBEAM_TYPE_* by torch's type
 
 
 def _need(t, dtype, name, dev):
@@ -578,7 +578,9 @@ def _rows_of(x, lengths, name):
     """(ctcbeam_rows, B, T, W, device) of scores [B, T, W] with adjacent labels."""
     import torch
     _need(x, None, name, getattr(x, "device", None))
-    code = _TYPES.get(str(x.dtype))
+    if not _TYPES:
+        _TYPES.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2})
+    code = _TYPES.get(x.dtype)
     if code is None:
         raise TypeError(f"{name} must be float32, float16 or bfloat16, got {x.dtype}")
     if x.dim() != 3:
@@ -592,6 +594,15 @@ def _rows_of(x, lengths, name):
                  _pointer(lengths, torch.int32, "lengths", (B,), dev)), B, T, W, dev
 
 
+def _output(t, dtype, name, shape, like, owned):
+    """(tensor, address) of an output: the given one, or a new one."""
+    if t is None:
+        t = like.new_empty(shape, dtype=dtype)
+        owned.append(t)
+        return t, t.data_ptr()
+    return t, _pointer(t, dtype, name, shape, like.device)
+
+
 def _workspace(workspace, need, dev, owned):
     """(tensor or None, address, bytes): the given workspace, or one of ``need`` bytes."""
     import torch
@@ -600,6 +611,7 @@ def _workspace(workspace, need, dev, owned):
             return None, None, 0
         workspace = torch.empty((need,), dtype=torch.uint8, device=dev)
         owned.append(workspace)
+        return workspace, workspace.data_ptr(), need
     return workspace, _dptr(workspace, torch.uint8, "workspace", None, dev), workspace.numel()
 
 
@@ -625,7 +637,7 @@ def ctcbeam_process_logits(logits, lengths=None, history=None, history_lengths=N
     lib = _load()
     rows, B, T, W, dev = _rows_of(logits, lengths, "logits")
     owned = []
-    out = _alloc(out, (B, T, W), torch.float32, dev, owned)
+    out, op = _output(out, torch.float32, "out", (B, T, W), logits, owned)
     o = _ProcessOpts(repetition=repetition, presence=presence, frequency=frequency, normalize=bool(normalize))
     if history is not None:
         _need(history, torch.int32, "history", dev)
@@ -659,7 +671,6 @@ def ctcbeam_process_logits(logits, lengths=None, history=None, history_lengths=N
         o.mask_stride_b = mask.stride(0) if mask.dim() > 1 else 0
         o.mask_stride_t = mask.stride(1) if mask.dim() > 2 else 0
     workspace, wp, wn = _workspace(workspace, lib.ctcbeam_process_workspace_bytes(B, T, W), dev, owned)
-    op = _pointer(out, torch.float32, "out", (B, T, W), dev)
     _launch(lambda st: lib.ctcbeam_process_logits(ctypes.byref(rows), ctypes.byref(o), op, wp, wn, st),
             dev, stream, owned)
     return out, workspace
@@ -679,13 +690,10 @@ def ctcbeam_top_logits(logits, k: int, lengths=None, temperature: float = 1.0, v
     k = int(k)
     owned = []
     kk = max(k, 0)
-    values = _alloc(values, (B, T, kk), torch.float32, dev, owned)
-    ids = _alloc(ids, (B, T, kk), torch.int32, dev, owned)
-    tail = _alloc(tail, (B, T), torch.float32, dev, owned)
+    values, vp = _output(values, torch.float32, "values", (B, T, kk), logits, owned)
+    ids, ip = _output(ids, torch.int32, "ids", (B, T, kk), logits, owned)
+    tail, tp = _output(tail, torch.float32, "tail", (B, T), logits, owned)
     workspace, wp, wn = _workspace(workspace, lib.ctcbeam_top_workspace_bytes(B, T, W, k), dev, owned)
-    vp = _pointer(values, torch.float32, "values", (B, T, kk), dev)
-    ip = _pointer(ids, torch.int32, "ids", (B, T, kk), dev)
-    tp = _pointer(tail, torch.float32, "tail", (B, T), dev)
     _launch(lambda st: lib.ctcbeam_top_logits(ctypes.byref(rows), k, temperature, vp, ip, tp, wp, wn, st),
             dev, stream, owned)
     return values, ids, tail, workspace
@@ -727,10 +735,8 @@ def ctcbeam_distill(student, values, ids, tail=None, lengths=None, temperature: 
     lp = gp = None
     gsb = gst = 0
     if want_loss or loss is not None:
-        loss = _alloc(loss, (B, T), torch.float32, dev, owned)
-        lp = _pointer(loss, torch.float32, "loss", (B, T), dev)
-    if want_grad or grad is not None:
-        grad = _alloc(grad, (B, T, W), student.dtype, dev, owned)
+        loss, lp = _output(loss, torch.float32, "loss", (B, T), student, owned)
+    if grad is not None:
         _need(grad, student.dtype, "grad", dev)
         if grad.shape != (B, T, W):
             raise ValueError(f"grad must have shape {(B, T, W)}, got {tuple(grad.shape)}")
@@ -738,6 +744,9 @@ def ctcbeam_distill(student, values, ids, tail=None, lengths=None, temperature: 
         if W > 1 and gsl != 1:
             raise ValueError("the labels of a row of grad must be adjacent")
         gp = grad.data_ptr()
+    elif want_grad:
+        grad, gp = _output(None, student.dtype, "grad", (B, T, W), student, owned)
+        gsb, gst = T * W, W
     workspace, wp, wn = _workspace(workspace, lib.ctcbeam_distill_workspace_bytes(B, T, W), dev, owned)
     _launch(lambda st: lib.ctcbeam_distill(ctypes.byref(rows), vp, ip, tp, k, temperature, w, wsb, wst, weight,
                                            lp, gp, gsb, gst, wp, wn, st), dev, stream, owned)

@@ -256,21 +256,24 @@ struct RawRow {
   // f(value, label, there) for the labels of this thread, by all threads alike:
   // `there` is false behind the last label
   template <typename Fn>
-  __device__ __forceinline__ void every(const L& lay, Fn f) const {
+  __device__ __forceinline__ void every(const L& lay, Fn f) {
 #pragma unroll
     for (int i = 0; i < L::kVecs; ++i)
       if (i < lay.vecs) {
+        forget(i);
         float v[L::kVec];
         unpack(raw[i], v, T());
+        int label = lay.vec_label(i);
+        asm volatile("" : "+v"(label));  // (nor are all the labels kept)
 #pragma unroll
-        for (int e = 0; e < L::kVec; ++e) f(v[e], lay.vec_label(i) + e, true);
+        for (int e = 0; e < L::kVec; ++e) f(v[e], label + e, true);
       }
 #pragma unroll
     for (int j = 0; j < L::kVec; ++j)
       if (j < lay.left) f(to_float(one[j]), lay.left_label(j), lay.left_label(j) < lay.W);
   }
   template <typename Fn>
-  __device__ __forceinline__ void each(const L& lay, Fn f) const {
+  __device__ __forceinline__ void each(const L& lay, Fn f) {
     every(lay, [&](float v, int label, bool there) {
       if (there) f(v, label);
     });
@@ -304,9 +307,13 @@ struct RawRow {
   // otherwise derived) values of all labels in registers from before.
   __device__ __forceinline__ void forget() {
 #pragma unroll
-    for (int i = 0; i < L::kVecs; ++i)
+    for (int i = 0; i < L::kVecs; ++i) forget(i);
+  }
+  // The same for one vector, in the order of the program: its values are not
+  // unpacked while others are still worked on.
+  __device__ __forceinline__ void forget(int i) {
 #pragma unroll
-      for (int w = 0; w < 4; ++w) asm volatile("" : "+v"(raw[i].w[w]));
+    for (int w = 0; w < 4; ++w) asm volatile("" : "+v"(raw[i].w[w]));
   }
 };
 

@@ -20,9 +20,9 @@ namespace ctcbeam {
 namespace rows {
 
 struct TopPlan {
-  int n, f;   // threads of a row (of a span), labels of a thread
-  int spans;  // per row
-  int span;   // labels of a span (the last one may hold fewer)
+  int n, vecs;  // threads of a row (of a span), vectors of 16 bytes of a thread
+  int spans;    // per row
+  int span;     // labels of a span (the last one may hold fewer)
 };
 
 // what a span leaves for the second launch: k keys, descending (0: none), and
@@ -41,40 +41,57 @@ __device__ __forceinline__ int key_label(uint64_t key) { return static_cast<int>
 constexpr uint32_t kOrderNegInf = 0x007FFFFFu;  // order32(-inf)
 constexpr float kTooSmall = 0x1p-80f;           // a sum that its reference may have pushed below fp32
 
-// Places above the largest bound of 16 leading bits that at least k of n keys
-// reach; 4 keys a lane (of all zeros where there is none).
+// The largest bound of 16 leading bits that at least k of the keys reach, PER
+// keys a lane.
 template <int PER>
 __device__ __forceinline__ uint32_t bound_of(const uint32_t* keys, int k) {
-  uint32_t bound = 0;
+  uint32_t own[PER], bound = 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) own[i] = keys[i * 64];
 #pragma unroll
   for (int bit = 31; bit >= 16; --bit) {
     const uint32_t t = bound | (1u << bit);
     int n = 0;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) n += __popcll(__ballot(keys[i] >= t));
+    for (int i = 0; i < PER; ++i) n += __popcll(__ballot(own[i] >= t));
     if (n >= k) bound = t;
   }
   return bound;
 }
 
-template <typename T, int N, int F, bool PART>
-__global__ void __launch_bounds__(N > kThreads ? N : kThreads) top_kernel(const TopParams p, const TopPlan plan, void* ws) {
-  using L = Layout<T, N, F>;
-  constexpr int kTeams = N > kThreads ? 1 : kThreads / N;
-  constexpr int kMaxima = N == 64 ? 64 : 256;  // groups whose maxima give the bound
-  constexpr int kRoom = 4 * N, kOwn = kRoom / N;
+template <int CTRL>
+__device__ __forceinline__ float max_dpp(float v) {
+  return fmaxf(v, __uint_as_float(detail::dpp_full<CTRL>(__float_as_uint(v))));
+}
+// the maximum of each `group` lanes (a power of two up to 16), in all of them
+__device__ __forceinline__ float group_max(float v, int group) {
+  if (group > 1) v = max_dpp<detail::kDppQuadXor1>(v);
+  if (group > 2) v = max_dpp<detail::kDppQuadXor2>(v);
+  if (group > 4) v = max_dpp<0x141>(v);
+  if (group > 8) v = max_dpp<0x140>(v);
+  return v;
+}
+
+template <typename T, int N, int VECS, bool PART>
+__global__ void __launch_bounds__(N > kThreads ? N : kThreads) __attribute__((amdgpu_waves_per_eu(VECS == 16 ? 4 : 1)))
+top_kernel(const TopParams p, const TopPlan plan, void* ws) {
+  using L = Layout<T, N, VECS * Packed<T>::kVec>;
+  constexpr int V = L::kVec, kTeams = N > kThreads ? 1 : kThreads / N;
+  constexpr int kRoom = N == 64 ? 256 : 1024, kOwn = kRoom / N;
+  static_assert(N > 64 || (VECS + 1) * V <= 64, "a lane's labels as bits");
   __shared__ float red_all[kTeams][4][N / 64];
   __shared__ __align__(16) uint64_t room_all[kTeams][kRoom + 2];
-  __shared__ uint32_t maxima[N == 64 ? 1 : kMaxima];
+  __shared__ uint32_t maxima[N == 64 ? 1 : 256];
   __shared__ int found_lds;
+  __shared__ uint32_t bound_lds;
   __shared__ uint64_t last_all[kTeams];
   const int tid = threadIdx.x % N, team = team_of<N>(), lane = threadIdx.x & 63;
   Team<N> tm(red_all[team]);
   uint64_t* room = room_all[team];
-  const uint32_t at = blockIdx.x * kTeams + team, T_ = p.in.T;
-  if (at >= p.in.B * T_) return;  // (a wave's row: no barrier is passed below)
-  const int b = at / T_, t = at % T_;
-  const int64_t row = at;
+  const uint32_t at_row = blockIdx.x * kTeams + team, T_ = p.in.T;
+  if (at_row >= p.in.B * T_) return;  // (a wave's row: no barrier is passed below)
+  const int b = at_row / T_, t = at_row % T_;
+  const int64_t row = at_row;
   if (t >= length_of(p.in, b)) {
     if (!PART) {
       for (int i = tid; i < p.k; i += N) {
@@ -88,29 +105,30 @@ __global__ void __launch_bounds__(N > kThreads ? N : kThreads) top_kernel(const 
   const int span = PART ? blockIdx.y : 0, c0 = PART ? span * plan.span : 0;
   const L lay(PART ? min(p.in.W - c0, plan.span) : p.in.W, tid);
   const int k = PART ? min(p.k, lay.W) : p.k;
-  RawRow<T, N, F> x(lay, static_cast<const T*>(p.in.data) + b * p.in.stride_b + t * p.in.stride_t + c0);
+  const T* in = static_cast<const T*>(p.in.data) + b * p.in.stride_b + t * p.in.stride_t + c0;
+  RawRow<T, N, VECS * V> x(lay, in);
 
-  // the bound
-  float mx = kNegInf;
-  x.each(lay, [&](float v, int) { mx = fmaxf(mx, v); });
-  mx = clean(mx);
+  // the bound (a maximum that a signalling NaN has spoilt only makes it lower)
+  const float mx = clean(x.largest(lay));
   uint32_t bound;
   if constexpr (N == 64) {
     const uint32_t key = order32(mx);
     bound = bound_of<1>(&key, k);
   } else {
-    if constexpr (N > 256) {
-      mx = fmaxf(mx, __uint_as_float(detail::dpp_full<detail::kDppQuadXor1>(__float_as_uint(mx))));
-      if constexpr (N > 512) mx = fmaxf(mx, __uint_as_float(detail::dpp_full<detail::kDppQuadXor2>(__float_as_uint(mx))));
-    }
-    constexpr int per = N / kMaxima;
-    if (tid % per == 0) maxima[tid / per] = order32(mx);
+    // twice as many groups as places in the list, or 256; those of short rows
+    // are single threads, so that k of them have a label
+    const int groups = lay.vecs == 0 || k > 64 ? 256 : k > 32 ? 128 : 64, per = N / groups;
+    const float g = group_max(mx, per);
+    if (tid % per == 0) maxima[tid / per] = order32(g);
     if (tid == 0) found_lds = 0;
     __syncthreads();
-    uint32_t keys[kMaxima / 64];
-#pragma unroll
-    for (int i = 0; i < kMaxima / 64; ++i) keys[i] = maxima[lane + 64 * i];
-    bound = bound_of<kMaxima / 64>(keys, k);
+    if (tid < 64) {
+      const uint32_t* keys = maxima + lane;
+      bound = groups == 64 ? bound_of<1>(keys, k) : groups == 128 ? bound_of<2>(keys, k) : bound_of<4>(keys, k);
+      if (tid == 0) bound_lds = bound;
+    }
+    __syncthreads();
+    bound = bound_lds;
   }
   float t0 = bound <= kOrderNegInf ? kNegInf : from_order32(bound);
 
@@ -118,34 +136,93 @@ __global__ void __launch_bounds__(N > kThreads ? N : kThreads) top_kernel(const 
   const float c = p.scale * kLog2e;
   float low = 0.0f;
   int n = 0;
-  const auto put = [&](bool take, float v, int label) {
-    if constexpr (N == 64) {
-      const uint64_t who = __ballot(take);
-      if (who) {
-        const int at = n + __popcll(who & detail::lanemask_lt());
-        if (take && at < kRoom) room[at] = detail::order_key(clean(v), c0 + label);
-        n += __popcll(who);
-      }
-    } else if (take) {
-      const int at = atomicAdd(&found_lds, 1);
-      if (at < kRoom) room[at] = detail::order_key(clean(v), c0 + label);
-    }
+  const auto put = [&](float v, int label) {
+    const int at = atomicAdd(&found_lds, 1);
+    if (at < kRoom) room[at] = detail::order_key(clean(v), c0 + label);
   };
   const auto found = [&]() {
     if constexpr (N > 64) {
       __syncthreads();
       n = found_lds;
     }
-    return n;
   };
-  x.forget();
-  x.every(lay, [&](float v, int label, bool there) {
-    v = fmaxf(v, kNegInf);
-    const bool take = there && v >= t0;
-    put(take, v, label);
-    low += take || !there ? 0.0f : exp2_((v - t0) * c);
-  });
-  if (found() > kRoom) {
+  {
+    const float shift = t0 * c;  // (one rounding, the same for all: within that of the result)
+    x.forget();
+    if constexpr (N == 64) {
+      // a lane's taken labels as bits; places by a sum over the lanes before
+      uint64_t taken = 0;
+#pragma unroll
+      for (int i = 0; i < VECS; ++i)
+        if (i < lay.vecs) {
+          x.forget(i);
+          float v[V];
+          unpack(x.raw[i], v, T());
+          uint32_t m = 0;
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            const bool take = v[e] >= t0;
+            m |= take ? 1u << e : 0u;
+            low += exp2_(take ? kNegInf : __builtin_fmaf(v[e], c, -shift));
+          }
+          taken |= static_cast<uint64_t>(m) << (i * V);
+        }
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        if (j >= lay.left) break;
+        const float v = lay.left_label(j) < lay.W ? to_float(x.one[j]) : __builtin_nanf("");
+        const bool take = v >= t0;
+        taken |= take ? 1ull << (VECS * V + j) : 0ull;
+        if (lay.left_label(j) < lay.W) low += exp2_(take ? kNegInf : __builtin_fmaf(v, c, -shift));
+      }
+      const int mine = __popcll(taken);
+      int at = detail::wave_incl_scan(mine, lane);
+      n = __builtin_amdgcn_readlane(at, 63);
+      at -= mine;
+      if (n <= kRoom) {
+        while (taken) {
+          const int bit = __ffsll(static_cast<unsigned long long>(taken)) - 1;
+          const int label = bit < VECS * V ? lay.vec_label(bit / V) + bit % V : lay.left_label(bit - VECS * V);
+          room[at++] = detail::order_key(clean(to_float(in[label])), label);
+          taken &= taken - 1;
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < VECS; ++i)
+        if (i < lay.vecs) {
+          x.forget(i);
+          float v[V];
+          unpack(x.raw[i], v, T());
+          bool any = false;
+#pragma unroll
+          for (int e = 0; e < V; ++e) any |= v[e] >= t0;
+          if (__ballot(any)) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+              if (v[e] >= t0) put(v[e], lay.vec_label(i) + e);
+              else low += exp2_(__builtin_fmaf(v[e], c, -shift));
+            }
+          } else {
+#pragma unroll
+            for (int e = 0; e < V; ++e) low += exp2_(__builtin_fmaf(v[e], c, -shift));
+          }
+        }
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        if (j >= lay.left) break;
+        if (lay.left_label(j) < lay.W) {
+          const float v = to_float(x.one[j]);
+          if (v >= t0) put(v, lay.left_label(j));
+          else low += exp2_(__builtin_fmaf(v, c, -shift));
+        }
+      }
+      found();
+    }
+  }
+  // More labels than there is room for, or (where threads have none, or NaN)
+  // no bound, or fewer than k above it: the k-th is found exactly.
+  if (n > kRoom || n < k || t0 == kNegInf) {
     const auto count = [&](auto which) {
       float mine = 0.0f;  // whole numbers below 2^24: exact
       x.forget();
@@ -154,93 +231,90 @@ __global__ void __launch_bounds__(N > kThreads ? N : kThreads) top_kernel(const 
     };
     uint32_t kth = 0;
     for (int bit = 31; bit >= 0; --bit) {
-      const uint32_t t = kth | (1u << bit);
-      if (count([&](uint32_t u, int) { return u >= t; }) >= k) kth = t;
+      const uint32_t u = kth | (1u << bit);
+      if (count([&](uint32_t o, int) { return o >= u; }) >= k) kth = u;
     }
-    const int ties = k - count([&](uint32_t u, int) { return u > kth; });
+    const int ties = k - count([&](uint32_t o, int) { return o > kth; });
     int last = 0;  // the label of the last tie that is listed
     for (int bit = 17; bit >= 0; --bit) {
-      const int t = last | (1 << bit);
-      if (count([&](uint32_t u, int label) { return u == kth && label < t; }) < ties) last = t;
+      const int l = last | (1 << bit);
+      if (count([&](uint32_t o, int label) { return o == kth && label < l; }) < ties) last = l;
     }
-    if constexpr (N > 64) {
-      if (tid == 0) found_lds = 0;
-      __syncthreads();
-    }
-    n = 0;
+    tm.sync();
+    if (tid == 0) found_lds = 0;
+    tm.sync();
     low = 0.0f;
     t0 = from_order32(kth);
     x.forget();
+    int at = 0;  // (a wave's places: counted by all lanes alike)
     x.every(lay, [&](float v, int label, bool there) {
       v = clean(v);
-      const uint32_t u = order32(v);
-      const bool take = there && (u > kth || (u == kth && label <= last));
-      put(take, v, label);
+      const uint32_t o = order32(v);
+      const bool take = there && (o > kth || (o == kth && label <= last));
+      if constexpr (N == 64) {
+        const uint64_t who = __ballot(take);
+        if (take) room[at + __popcll(who & detail::lanemask_lt())] = detail::order_key(v, label);
+        at += __popcll(who);
+      } else {
+        if (take) put(v, label);
+      }
       low += take || !there || !(v > kNegInf) ? 0.0f : exp2_((v - t0) * c);
     });
+    n = k;
     found();
   }
 
-  // each label's place is the number of larger keys
+  // each label's place is the number of larger keys; those behind the list
+  // belong to the sum
   if (tid < 2) room[n + tid] = 0;
   tm.sync();
-  float beside[kOwn];
-#pragma unroll
-  for (int i = 0; i < kOwn; ++i) {
-    beside[i] = kNegInf;
-    const int at = tid + i * N;
-    if (at < n) {
-      const uint64_t key = room[at];
-      int place = 0;
-      for (int j = 0; j < n; j += 2) {
-        const uint64_t a = room[j], d = room[j + 1];
-        place += (a > key) + (d > key);
-      }
-      if (place == k - 1) last_all[team] = key;
-      if (place >= k) {
-        beside[i] = key_value(key);
-      } else if (PART) {
-        span_keys(ws, row, plan.spans, span, p.k)[place] = key;
-      } else {
-        p.values[row * p.k + place] = key_value(key);
-        p.ids[row * p.k + place] = key_label(key);
-      }
+#pragma unroll 1
+  for (int at = tid; at < n; at += N) {
+    const uint64_t key = room[at];
+    int place = 0;
+    for (int j = 0; j < n; j += 2) {
+      const uint64_t a = room[j], d = room[j + 1];
+      place += (a > key) + (d > key);
+    }
+    if (place == k - 1) last_all[team] = key;
+    if (place >= k) {
+      low += exp2_((key_value(key) - t0) * c);
+    } else if (PART) {
+      span_keys(ws, row, plan.spans, span, p.k)[place] = key;
+    } else {
+      p.values[row * p.k + place] = key_value(key);
+      p.ids[row * p.k + place] = key_label(key);
     }
   }
-  tm.sync();
-  const uint64_t last = last_all[team];
-  float ref = key_value(last), s = 0.0f;
-  if (ref > kNegInf) {
-    s = low > 0.0f ? low * exp2_((t0 - ref) * c) : 0.0f;
-#pragma unroll
-    for (int i = 0; i < kOwn; ++i) s += exp2_((beside[i] - ref) * c);
-    s = tm.sum(s);
-    if (s < kTooSmall && k < lay.W) {
-      // what is left lies far below the list: relative to its own maximum
-      float m = kNegInf;
+  float ref = t0, s = tm.sum(low);
+  if (!(s >= kTooSmall && s < kLargest) && k < lay.W) {
+    // what is left lies far from the bound, or there is NaN among it: relative to its own maximum
+    tm.sync();
+    const uint64_t last = last_all[team];
+    float m = kNegInf;
+    x.forget();
+    x.each(lay, [&](float v, int label) {
+      v = clean(v);
+      if (detail::order_key(v, c0 + label) < last) m = fmaxf(m, v);
+    });
+    ref = tm.max(m);
+    s = 0.0f;
+    if (ref > kNegInf) {
       x.forget();
       x.each(lay, [&](float v, int label) {
         v = clean(v);
-        if (detail::order_key(v, c0 + label) < last) m = fmaxf(m, v);
+        if (detail::order_key(v, c0 + label) < last) s += exp2_((v - ref) * c);
       });
-      ref = tm.max(m);
-      s = 0.0f;
-      if (ref > kNegInf) {
-        x.forget();
-        x.each(lay, [&](float v, int label) {
-          v = clean(v);
-          if (detail::order_key(v, c0 + label) < last) s += exp2_((v - ref) * c);
-        });
-        s = tm.sum(s);
-      }
+      s = tm.sum(s);
     }
   }
+  const bool some = k < lay.W && s > 0.0f;
   if (PART) {
     uint64_t* keys = span_keys(ws, row, plan.spans, span, p.k);
     for (int i = k + tid; i < p.k; i += N) keys[i] = 0;
-    if (tid == 0) *reinterpret_cast<Part*>(keys + p.k) = {s > 0.0f ? ref : kNegInf, s};
+    if (tid == 0) *reinterpret_cast<Part*>(keys + p.k) = {some ? ref : kNegInf, some ? s : 0.0f};
   } else if (tid == 0) {
-    p.tail[row] = s > 0.0f ? ref * p.scale + logf(s) : kNegInf;
+    p.tail[row] = some ? ref * p.scale + logf(s) : kNegInf;
   }
 }
 
@@ -309,47 +383,68 @@ __global__ void __launch_bounds__(kThreads) join_top_kernel(const TopParams p, c
   if (tid == 0) p.tail[row] = s > 0.0f ? m * p.scale + logf(s) : kNegInf;
 }
 
-static TopPlan plan_top(int B, int T, int W, int k) {
+static TopPlan plan_top(int type, int B, int T, int W, int k) {
   const int64_t rows = static_cast<int64_t>(B) * T;
-  if (W < 64 * 36 && k <= 32 && rows >= 1024) return {64, W < 64 * 20 ? 16 : 32, 1, W};
-  if (W < 256 * 36) return {256, W < 256 * 12 ? 8 : W < 256 * 20 ? 16 : 32, 1, W};
+  const int vec = type == kTypeF32 ? 4 : 8;
+  // threads and their vectors, by what they hold: N * (vecs + 1) * vec - 1 labels
+  const auto holds = [&](int n, int vecs) { return W < n * (vecs + 1) * vec; };
+  if (k <= 32 && rows >= 1024 && W < 64 * 36) return {64, holds(64, 16 / vec) ? 16 / vec : 32 / vec, 1, W};
+  if (holds(256, 4)) return {256, holds(256, 1) ? 1 : holds(256, 2) ? 2 : 4, 1, W};
+  if (rows >= 512) {
+    if (holds(256, 16)) return {256, holds(256, 8) ? 8 : 16, 1, W};
+    if (holds(512, 16)) return {512, 16, 1, W};
+  }
+  if (holds(1024, 16)) return {1024, holds(1024, 4) ? 4 : holds(1024, 8) ? 8 : 16, 1, W};
   // equal spans of what a workgroup of 1024 holds
-  const int most = 1024 * 36 - 1, spans = (W + most - 1) / most;
-  const int span = ((W + spans - 1) / spans + 63) / 64 * 64;
-  return {1024, 32, spans, std::min(span, W)};
+  const int most = 1024 * 17 * vec - 1, spans = (W + most - 1) / most;
+  return {1024, 16, spans, ((W + spans - 1) / spans + 63) / 64 * 64};
 }
 
-template <typename T, int N, int F>
+template <typename T, int N, int VECS>
 static void run_top(const TopParams& p, const TopPlan& q, void* ws, hipStream_t stream) {
   constexpr int threads = N > kThreads ? N : kThreads;
-  const int64_t rows = static_cast<int64_t>(p.in.B) * p.in.T;
-  if constexpr (N == 1024) {
+  const uint32_t rows = static_cast<uint32_t>(p.in.B) * p.in.T;
+  if constexpr (N == 1024 && VECS == 16) {
     if (q.spans > 1) {
-      top_kernel<T, N, F, true><<<dim3(static_cast<uint32_t>(rows), q.spans), threads, 0, stream>>>(p, q, ws);
-      join_top_kernel<<<static_cast<uint32_t>(rows), kThreads, sizeof(uint64_t) * q.spans * p.k, stream>>>(p, q, ws);
+      top_kernel<T, N, VECS, true><<<dim3(rows, q.spans), threads, 0, stream>>>(p, q, ws);
+      join_top_kernel<<<rows, kThreads, sizeof(uint64_t) * q.spans * p.k, stream>>>(p, q, ws);
       return;
     }
   }
-  const int64_t per = threads / N;
-  top_kernel<T, N, F, false><<<static_cast<uint32_t>((rows + per - 1) / per), threads, 0, stream>>>(p, q, ws);
+  constexpr uint32_t per = threads / N;
+  top_kernel<T, N, VECS, false><<<(rows + per - 1) / per, threads, 0, stream>>>(p, q, ws);
 }
 
 template <typename T>
 static hipError_t choose_top(const TopParams& p, void* ws, hipStream_t stream) {
-  const TopPlan q = plan_top(p.in.B, p.in.T, p.in.W, p.k);
-  if (q.n == 64) q.f == 16 ? run_top<T, 64, 16>(p, q, ws, stream) : run_top<T, 64, 32>(p, q, ws, stream);
-  else if (q.n == 1024) run_top<T, 1024, 32>(p, q, ws, stream);
-  else if (q.f == 8) run_top<T, 256, 8>(p, q, ws, stream);
-  else if (q.f == 16) run_top<T, 256, 16>(p, q, ws, stream);
-  else run_top<T, 256, 32>(p, q, ws, stream);
+  constexpr int V = Packed<T>::kVec;
+  const TopPlan q = plan_top(p.in.type, p.in.B, p.in.T, p.in.W, p.k);
+  if (q.n == 64) q.vecs == 16 / V ? run_top<T, 64, 16 / V>(p, q, ws, stream) : run_top<T, 64, 32 / V>(p, q, ws, stream);
+  else if (q.n == 512) run_top<T, 512, 16>(p, q, ws, stream);
+  else if (q.n == 1024) {
+    if (q.vecs == 4) run_top<T, 1024, 4>(p, q, ws, stream);
+    else if (q.vecs == 8) run_top<T, 1024, 8>(p, q, ws, stream);
+    else run_top<T, 1024, 16>(p, q, ws, stream);
+  } else {
+    if (q.vecs == 1) run_top<T, 256, 1>(p, q, ws, stream);
+    else if (q.vecs == 2) run_top<T, 256, 2>(p, q, ws, stream);
+    else if (q.vecs == 4) run_top<T, 256, 4>(p, q, ws, stream);
+    else if (q.vecs == 8) run_top<T, 256, 8>(p, q, ws, stream);
+    else run_top<T, 256, 16>(p, q, ws, stream);
+  }
   return hipGetLastError();
 }
 
 }  // namespace rows
 
+// (for either width of the scores, as the caller need not say it)
 size_t top_workspace(int B, int T, int W, int k) {
-  const rows::TopPlan q = rows::plan_top(B, T, W, k);
-  return q.spans == 1 ? 0 : static_cast<size_t>(B) * T * q.spans * (k + 1) * sizeof(uint64_t);
+  size_t most = 0;
+  for (int type : {kTypeF32, kTypeBF16}) {
+    const rows::TopPlan q = rows::plan_top(type, B, T, W, k);
+    if (q.spans > 1) most = std::max(most, static_cast<size_t>(B) * T * q.spans * (k + 1) * sizeof(uint64_t));
+  }
+  return most;
 }
 
 hipError_t launch_top(const TopParams& p, void* workspace, hipStream_t stream) {

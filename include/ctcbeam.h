@@ -338,7 +338,7 @@ typedef struct ctcbeam_process_opts {
  * result is what the decode calls take as log-probabilities.  Per label c,
  * with n the occurrences of c in the utterance's history, in fp32:
  *   x = logit (NaN: -inf; +inf: the largest finite number)
- *   if n > 0: x = x > 0 ? x / repetition : x * repetition;
+ *   if n > 0: x = x > 0 ? x * (1 / repetition) : x * repetition;
  *             x = (x - frequency * n) - presence
  *   x = x + bias[c] (NaN: -inf; +inf: the largest finite number)
  *   a barred label: x = -inf

@@ -41,8 +41,8 @@ KERNEL_UNITS = ["ctcbeam_kernel_lpt1.hip", "ctcbeam_kernel_lpt2.hip", "ctcbeam_k
                 "ctcbeam_kernel_lpt4_rep.hip", "ctcbeam_kernel_lpt8_rep.hip", "ctcbeam_class_lpt1.hip", "ctcbeam_class_lpt2.hip",
                 "ctcbeam_class_lpt4.hip", "ctcbeam_class_lpt8.hip", "ctcbeam_greedy_v256.hip", "ctcbeam_greedy_v1024.hip",
                 "ctcbeam_greedy_v4096.hip", "ctcbeam_workspace.hip",
-                "ctcbeam_noalloc.hip", "ctcbeam_small.hip", "ctcbeam_process.hip", "ctcbeam_top.hip",
-                "ctcbeam_distill.hip"]
+                "ctcbeam_noalloc.hip", "ctcbeam_small.hip",
+                *(f"ctcbeam_{op}_{t}.hip" for op in ("top", "distill", "process") for t in ("f32", "f16", "bf16"))]
 HOST_UNITS = ["ctcbeam_host.cpp", "ctcbeam_rows_host.cpp"]
 
 

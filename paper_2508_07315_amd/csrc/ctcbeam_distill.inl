@@ -21,27 +21,15 @@
 // out and put back.  Longer rows are held by a workgroup of 1024, in packed
 // registers, with a bit per label in LDS; or, where they are few or longer than
 // that, cut into spans whose sums a second launch joins.
-#include <algorithm>
+#pragma once
 
 #include "ctcbeam_rows_lane.h"
+#include "ctcbeam_rows_plan.h"
 
 namespace ctcbeam {
 namespace rows {
 
 enum DistillPhase { kOneLaunch = 0, kSpanSums = 1, kSpanGrads = 2 };
-
-struct DistillPlan {
-  int n, f;   // threads of a row (of a span), labels of a thread
-  int spans;  // per row; 0: a workgroup holds the row in packed registers
-  int span;   // labels of a span (the last one may hold fewer)
-};
-
-// What a span leaves for the second launch: the sum over its listed labels
-// relative to m, R relative to r, the listed labels' part of the loss but for
-// log S, and their probability.
-struct SpanSums {
-  float m, listed_sum, r, R, terms, listed;
-};
 
 // The teacher's list of a row, two entries a lane.
 struct List {
@@ -98,23 +86,25 @@ struct List {
   __device__ __forceinline__ void sum_equal_labels(int k) {
     const int lane = threadIdx.x & 63;
     float sum[2] = {0.0f, 0.0f};
-    bool first[2] = {true, true};
-    for (int i = 0; i < k; ++i) {
-      const int other = i < 64 ? __shfl(id[0], i) : __shfl(id[1], i - 64);
-      const float more = i < 64 ? __shfl(prob[0], i) : __shfl(prob[1], i - 64);
+    int first[2] = {kMaxTop, kMaxTop};
 #pragma unroll
-      for (int e = 0; e < 2; ++e)
-        if (other == id[e]) {
-          sum[e] += more;
-          if (i < lane + 64 * e) first[e] = false;
+    for (int h = 0; h < 2; ++h)
+      for (int i = 0; i < k - 64 * h && i < 64; ++i) {
+        const int other = detail::rdlane(id[h], i);
+        const float more = detail::rdlane(prob[h], i);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const bool equal = other == id[e];
+          sum[e] += equal ? more : 0.0f;
+          first[e] = min(first[e], equal ? i + 64 * h : kMaxTop);
         }
-    }
+      }
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       if (id[e] < 0) continue;
       prob[e] = sum[e];
       log_prob[e] = logf(sum[e]);
-      if (!first[e]) id[e] = -1;
+      if (first[e] != lane + 64 * e) id[e] = -1;
     }
   }
 
@@ -349,6 +339,9 @@ distill_kernel(const DistillParams p, const DistillPlan plan, SpanSums* sums) {
 // label at the first free one from its own on.  One workgroup fills a compute unit, so reading,
 // computing and writing overlap between units, not within one.
 constexpr int kPlaces = 4 * kMaxTop;
+static_assert(kPlaces == 512, "nine bits of the product");
+// a label's own place: labels at even distances do not meet in one
+__device__ __forceinline__ int place_of(int label) { return static_cast<int>(static_cast<uint32_t>(label) * 0x9E3779B1u >> 23); }
 
 template <typename T, int N, int VECS>
 __global__ void __launch_bounds__(N) distill_wide_kernel(const DistillParams p) {
@@ -396,7 +389,7 @@ __global__ void __launch_bounds__(N) distill_wide_kernel(const DistillParams p) 
     if (__ballot(again)) list.sum_equal_labels(p.k);
     list.each([&](int d) {
       if (list.id[d] < 0) return;
-      int at = list.id[d] % kPlaces;  // (at most kMaxTop labels: there is a free place)
+      int at = place_of(list.id[d]);  // (at most kMaxTop labels: there is a free place)
       while (atomicCAS(&place_label[at], -1, list.id[d]) != -1) at = (at + 1) % kPlaces;
       place[d] = at;
     });
@@ -465,7 +458,7 @@ __global__ void __launch_bounds__(N) distill_wide_kernel(const DistillParams p) 
   const float rest = of.rest_factor(w, c, rest_p);
   x.forget();
   const auto gradient_of = [&](int label) {
-    int at = label % kPlaces;  // (a listed label: it has a place)
+    int at = place_of(label);  // (a listed label: it has a place)
     while (place_label[at] != label) at = (at + 1) % kPlaces;
     return place_grad[at];
   };
@@ -495,23 +488,6 @@ __global__ void __launch_bounds__(N) distill_wide_kernel(const DistillParams p) 
   }
 }
 
-// Rows from which on a workgroup for each fills the card.
-constexpr int64_t kManyRows = 128;
-
-static DistillPlan plan_distill(int type, int B, int T, int W) {
-  const int64_t rows = static_cast<int64_t>(B) * T;
-  if (W < 64 * 36 && rows >= 1024) return {64, W < 64 * 20 ? 16 : 32, 1, W};
-  if (W < 256 * 36) return {256, W < 256 * 12 ? 8 : W < 256 * 20 ? 16 : 32, 1, W};
-  const int vec = type == kTypeF32 ? 4 : 8;
-  if (rows >= kManyRows && W < 1024 * 17 * vec) {
-    const int n = W < 256 * 17 * vec ? 256 : W < 512 * 17 * vec ? 512 : 1024;
-    return {n, (W < 256 * 9 * vec ? 8 : 16) * vec, 0, W};
-  }
-  int span = 8192;
-  while (span > 2048 && rows * ((W + span - 1) / span) < 512) span >>= 1;
-  return {256, span / 256, (W + span - 1) / span, span};
-}
-
 template <typename T, int N, int F>
 static void run_distill(const DistillParams& p, const DistillPlan& q, SpanSums* sums, hipStream_t stream) {
   constexpr int teams = kThreads / N;
@@ -529,13 +505,17 @@ static void run_distill(const DistillParams& p, const DistillPlan& q, SpanSums* 
 }
 
 template <typename T>
-static hipError_t choose_distill(const DistillParams& p, SpanSums* sums, hipStream_t stream) {
+static hipError_t launch_distill_impl(const DistillParams& p, void* workspace, hipStream_t stream) {
+  SpanSums* sums = static_cast<SpanSums*>(workspace);
   const DistillPlan q = plan_distill(p.in.type, p.in.B, p.in.T, p.in.W);
   const uint32_t rows = static_cast<uint32_t>(p.in.B) * p.in.T;
   if (q.spans == 0) {
-    if (q.n == 1024) distill_wide_kernel<T, 1024, 16><<<rows, 1024, 0, stream>>>(p);
+    const int vecs = q.f / Packed<T>::kVec;
+    if (q.n == 1024 && vecs == 4) distill_wide_kernel<T, 1024, 4><<<rows, 1024, 0, stream>>>(p);
+    else if (q.n == 1024 && vecs == 8) distill_wide_kernel<T, 1024, 8><<<rows, 1024, 0, stream>>>(p);
+    else if (q.n == 1024) distill_wide_kernel<T, 1024, 16><<<rows, 1024, 0, stream>>>(p);
     else if (q.n == 512) distill_wide_kernel<T, 512, 16><<<rows, 512, 0, stream>>>(p);
-    else if (q.f == 16 * Packed<T>::kVec) distill_wide_kernel<T, 256, 16><<<rows, 256, 0, stream>>>(p);
+    else if (vecs == 16) distill_wide_kernel<T, 256, 16><<<rows, 256, 0, stream>>>(p);
     else distill_wide_kernel<T, 256, 8><<<rows, 256, 0, stream>>>(p);
   } else if (q.n == 64) q.f == 16 ? run_distill<T, 64, 16>(p, q, sums, stream) : run_distill<T, 64, 32>(p, q, sums, stream);
   else if (q.f == 8) run_distill<T, 256, 8>(p, q, sums, stream);
@@ -545,22 +525,4 @@ static hipError_t choose_distill(const DistillParams& p, SpanSums* sums, hipStre
 }
 
 }  // namespace rows
-
-// (for either width of the scores, as the caller need not say it)
-size_t distill_workspace(int B, int T, int W) {
-  size_t most = 0;
-  for (int type : {kTypeF32, kTypeBF16}) {
-    const rows::DistillPlan q = rows::plan_distill(type, B, T, W);
-    if (q.spans > 1) most = std::max(most, static_cast<size_t>(B) * T * q.spans * sizeof(rows::SpanSums));
-  }
-  return most;
-}
-
-hipError_t launch_distill(const DistillParams& p, void* workspace, hipStream_t stream) {
-  rows::SpanSums* sums = static_cast<rows::SpanSums*>(workspace);
-  if (p.in.type == kTypeF32) return rows::choose_distill<float>(p, sums, stream);
-  if (p.in.type == kTypeF16) return rows::choose_distill<rows::F16>(p, sums, stream);
-  return rows::choose_distill<rows::BF16>(p, sums, stream);
-}
-
 }  // namespace ctcbeam

@@ -11,24 +11,19 @@
 //
 // The counts of the labels emitted before live in LDS, for the span that the
 // workgroup holds, and serve all its frames.
-#include <algorithm>
+#pragma once
 
 #include "ctcbeam_rows_lane.h"
+#include "ctcbeam_rows_plan.h"
 
 namespace ctcbeam {
 namespace rows {
 
 enum Phase { kWhole = 0, kStats = 1, kFinish = 2 };
 
-struct ProcessPlan {
-  int spans;   // per row
-  int span;    // labels of a span (the last one may hold fewer)
-  int frames;  // per workgroup
-  int groups;  // of frames, per utterance
-};
-
 template <typename T, int N, int F, int PHASE>
-__global__ void __launch_bounds__(kThreads) process_kernel(const ProcessParams p, const ProcessPlan plan, Part* parts) {
+__global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(F == 32 ? 4 : 1)))
+process_kernel(const ProcessParams p, const ProcessPlan plan, Part* parts) {
   using L = Layout<T, N, F>;
   constexpr int V = L::kVec;
   extern __shared__ uint32_t count[];
@@ -42,6 +37,13 @@ __global__ void __launch_bounds__(kThreads) process_kernel(const ProcessParams p
   const L lay(min(p.in.W - c0, plan.span), tid);
   Team<N> tm(red);
 
+  // the first row is on its way while the history is counted
+  const auto row_at = [&](int t) {
+    return static_cast<const T*>(p.in.data) + b * p.in.stride_b + t * p.in.stride_t + c0;
+  };
+  RawRow<T, N, F> raw;
+  if (t0 + team < T1) raw.load(lay, row_at(t0 + team));
+
   int H = p.H;
   float rep = 1.0f, pre = 0.0f, fre = 0.0f;
   if (H) {
@@ -50,13 +52,20 @@ __global__ void __launch_bounds__(kThreads) process_kernel(const ProcessParams p
     pre = p.penalties ? p.penalties[3 * b + 1] : p.presence;
     fre = p.penalties ? p.penalties[3 * b + 2] : p.frequency;
   }
+  const float per_rep = 1.0f / rep;  // (a quotient by way of it is off by a step and a half at most)
   if (H) {
     const int32_t* hist = p.history + b * p.history_stride;
-    for (int i = threadIdx.x; i < lay.W; i += kThreads) count[i] = 0;
+    for (int i = threadIdx.x * 4; i < lay.W; i += kThreads * 4) *reinterpret_cast<uint4*>(&count[i]) = uint4{0, 0, 0, 0};
     __syncthreads();
-    for (int i = threadIdx.x; i < H; i += kThreads) {
-      const uint32_t c = static_cast<uint32_t>(hist[i]) - static_cast<uint32_t>(c0);
-      if (c < static_cast<uint32_t>(lay.W)) atomicAdd(&count[c], 1u);
+    // four labels on their way at a time
+    for (int i = threadIdx.x; i < H; i += 4 * kThreads) {
+      uint32_t c[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        c[q] = i + q * kThreads < H ? static_cast<uint32_t>(hist[i + q * kThreads]) - static_cast<uint32_t>(c0) : ~0u;
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (c[q] < static_cast<uint32_t>(lay.W)) atomicAdd(&count[c[q]], 1u);
     }
     __syncthreads();
   }
@@ -64,16 +73,13 @@ __global__ void __launch_bounds__(kThreads) process_kernel(const ProcessParams p
 
   for (int t = t0 + team; t < T1; t += teams) {
     const int64_t row = static_cast<int64_t>(b) * p.in.T + t;
-    const T* in = static_cast<const T*>(p.in.data) + b * p.in.stride_b + t * p.in.stride_t + c0;
     const uint32_t* mask = p.mask ? p.mask + b * p.mask_stride_b + t * p.mask_stride_t + (c0 >> 5) : nullptr;
+    if (t >= t0 + teams) raw.load(lay, row_at(t));
     float x[F + V];
-    lay.load(in, x, kNegInf);
+    raw.values(lay, x);
     const auto seen = [&](float v, uint32_t n) {
-      if (n) {
-        v = v > 0.0f ? v / rep : v * rep;
-        v = clean((v - fre * static_cast<float>(n)) - pre);
-      }
-      return v;
+      const float w = clean((v * (v > 0.0f ? per_rep : rep) - fre * static_cast<float>(n)) - pre);
+      return n ? w : v;
     };
     float m = kNegInf;
 #pragma unroll
@@ -158,37 +164,6 @@ __global__ void __launch_bounds__(kThreads) process_kernel(const ProcessParams p
   }
 }
 
-// Labels of a row that one wave, and one workgroup, take whole: below
-// N * (F + 4), see Layout.
-constexpr int kRowOfWave = 64 * 36, kRowOfGroup = 256 * 36;
-
-static ProcessPlan plan_process(int B, int T, int W, bool normalize, int* n, int* f) {
-  const int64_t rows = static_cast<int64_t>(B) * T;
-  ProcessPlan q{1, W, 1, T};
-  if (W < kRowOfWave && rows >= 1024 && T >= 4) {
-    *n = 64;
-    *f = W < 64 * 20 ? 16 : 32;
-    q.frames = 4;
-  } else if (W < kRowOfGroup && (normalize || rows >= 512)) {
-    *n = 256;
-    *f = W < 256 * 12 ? 8 : W < 256 * 20 ? 16 : 32;
-  } else {
-    // spans: as long as the card stays full of them
-    int span = 8192;
-    while (span > 2048 && rows * ((W + span - 1) / span) < 512) span >>= 1;
-    *n = 256;
-    *f = span / 256;
-    q.spans = (W + span - 1) / span;
-    q.span = span;
-  }
-  // a workgroup's counts of past labels serve several frames where there are enough
-  const int64_t groups = rows * q.spans / q.frames;
-  const int more = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(16, groups / 2048)));
-  q.frames = std::min(q.frames * more, T);
-  q.groups = (T + q.frames - 1) / q.frames;
-  return q;
-}
-
 template <typename T, int N, int F>
 static hipError_t run_process(const ProcessParams& p, const ProcessPlan& q, Part* parts, hipStream_t stream) {
   const size_t lds = p.H ? sizeof(uint32_t) * ((std::min(q.span, p.in.W) + 3) / 4 * 4) : 0;
@@ -212,21 +187,12 @@ static hipError_t choose_process(const ProcessParams& p, const ProcessPlan& q, i
   return run_process<T, 256, 32>(p, q, parts, stream);
 }
 
+template <typename T>
+static hipError_t launch_process_impl(const ProcessParams& p, void* workspace, hipStream_t stream) {
+  int n, f;
+  const ProcessPlan q = plan_process(p.in.B, p.in.T, p.in.W, p.H, p.normalize != 0, &n, &f);
+  return choose_process<T>(p, q, n, f, static_cast<Part*>(workspace), stream);
+}
+
 }  // namespace rows
-
-size_t process_workspace(int B, int T, int W) {
-  int n, f;
-  const rows::ProcessPlan q = rows::plan_process(B, T, W, true, &n, &f);
-  return q.spans == 1 ? 0 : static_cast<size_t>(B) * T * q.spans * sizeof(rows::Part);
-}
-
-hipError_t launch_process(const ProcessParams& p, void* workspace, hipStream_t stream) {
-  int n, f;
-  const rows::ProcessPlan q = rows::plan_process(p.in.B, p.in.T, p.in.W, p.normalize != 0, &n, &f);
-  rows::Part* parts = static_cast<rows::Part*>(workspace);
-  if (p.in.type == kTypeF32) return rows::choose_process<float>(p, q, n, f, parts, stream);
-  if (p.in.type == kTypeF16) return rows::choose_process<rows::F16>(p, q, n, f, parts, stream);
-  return rows::choose_process<rows::BF16>(p, q, n, f, parts, stream);
-}
-
 }  // namespace ctcbeam

@@ -60,13 +60,26 @@ struct DistillParams {
   int64_t grad_stride_b, grad_stride_t;
 };
 
-// Workspaces in bytes; the launches use no more than these say.
-size_t process_workspace(int B, int T, int W);
-size_t top_workspace(int B, int T, int W, int k);
-size_t distill_workspace(int B, int T, int W);
+// By element type, in units of their own (`workspace`: what the plans need).
+#define CTCBEAM_ROW_LAUNCHES(type)                                                            \
+  hipError_t launch_process_##type(const ProcessParams& p, void* workspace, hipStream_t s);   \
+  hipError_t launch_top_##type(const TopParams& p, void* workspace, hipStream_t s);           \
+  hipError_t launch_distill_##type(const DistillParams& p, void* workspace, hipStream_t s);
+CTCBEAM_ROW_LAUNCHES(f32)
+CTCBEAM_ROW_LAUNCHES(f16)
+CTCBEAM_ROW_LAUNCHES(bf16)
+#undef CTCBEAM_ROW_LAUNCHES
 
-hipError_t launch_process(const ProcessParams& p, void* workspace, hipStream_t stream);
-hipError_t launch_top(const TopParams& p, void* workspace, hipStream_t stream);
-hipError_t launch_distill(const DistillParams& p, void* workspace, hipStream_t stream);
+// What the parts of a row leave in a workspace: a maximum and a sum of
+// exp2((x - max) * log2 e) ...
+struct Part {
+  float m, s;
+};
+// ... or, of a span of a student's row, the sum over its listed labels relative
+// to m, the others' R relative to r, the listed labels' part of the loss but
+// for log S, and their probability.
+struct SpanSums {
+  float m, listed_sum, r, R, terms, listed;
+};
 
 }  // namespace ctcbeam

@@ -9,6 +9,7 @@
 #include "../../include/ctcbeam.h"
 #include "ctcbeam_internal.h"
 #include "ctcbeam_rows.h"
+#include "ctcbeam_rows_plan.h"
 
 static_assert(CTCBEAM_TYPE_F32 == ctcbeam::kTypeF32 && CTCBEAM_TYPE_F16 == ctcbeam::kTypeF16 &&
                   CTCBEAM_TYPE_BF16 == ctcbeam::kTypeBF16,
@@ -99,6 +100,11 @@ bool sizes_fit(int B, int T, int W) {
   return B > 0 && T > 0 && W > 0 && W <= CTCBEAM_MAX_LABELS && static_cast<Wide>(B) * T <= CTCBEAM_MAX_ROWS;
 }
 
+template <typename F>
+F* by_type(int type, F* f32, F* f16, F* bf16) {
+  return type == CTCBEAM_TYPE_F32 ? f32 : type == CTCBEAM_TYPE_F16 ? f16 : bf16;
+}
+
 int device_there() {
   int dev = -1;
   return hipGetDevice(&dev) == hipSuccess ? 0 : refuse(4, "no HIP device");
@@ -108,16 +114,32 @@ int device_there() {
 
 extern "C" {
 
+// (for either width of the scores, as the caller does not say it)
 size_t ctcbeam_process_workspace_bytes(int B, int T, int W) {
-  return sizes_fit(B, T, W) ? ctcbeam::process_workspace(B, T, W) : 0;
+  if (!sizes_fit(B, T, W)) return 0;
+  int n, f;
+  const ctcbeam::rows::ProcessPlan q = ctcbeam::rows::plan_process(B, T, W, 0, true, &n, &f);
+  return q.spans == 1 ? 0 : static_cast<size_t>(B) * T * q.spans * sizeof(ctcbeam::Part);
 }
 
 size_t ctcbeam_top_workspace_bytes(int B, int T, int W, int k) {
-  return sizes_fit(B, T, W) && k > 0 && k <= CTCBEAM_MAX_TOP ? ctcbeam::top_workspace(B, T, W, k) : 0;
+  if (!sizes_fit(B, T, W) || k < 1 || k > CTCBEAM_MAX_TOP) return 0;
+  size_t most = 0;
+  for (int type : {CTCBEAM_TYPE_F32, CTCBEAM_TYPE_BF16}) {
+    const int spans = ctcbeam::rows::plan_top(type, B, T, W, k).spans;
+    if (spans > 1) most = std::max(most, static_cast<size_t>(B) * T * spans * (k + 1) * sizeof(uint64_t));
+  }
+  return most;
 }
 
 size_t ctcbeam_distill_workspace_bytes(int B, int T, int W) {
-  return sizes_fit(B, T, W) ? ctcbeam::distill_workspace(B, T, W) : 0;
+  if (!sizes_fit(B, T, W)) return 0;
+  size_t most = 0;
+  for (int type : {CTCBEAM_TYPE_F32, CTCBEAM_TYPE_BF16}) {
+    const int spans = ctcbeam::rows::plan_distill(type, B, T, W).spans;
+    if (spans > 1) most = std::max(most, static_cast<size_t>(B) * T * spans * sizeof(ctcbeam::SpanSums));
+  }
+  return most;
 }
 
 int ctcbeam_process_logits(const ctcbeam_rows* logits, const ctcbeam_process_opts* opts, float* out, void* workspace,
@@ -179,7 +201,7 @@ int ctcbeam_process_logits(const ctcbeam_rows* logits, const ctcbeam_process_opt
   p.mask_stride_t = o.mask_stride_t;
   p.normalize = o.normalize != 0;
   p.out = out;
-  return launched(ctcbeam::launch_process(p, workspace, stream));
+  return launched(by_type(p.in.type, ctcbeam::launch_process_f32, ctcbeam::launch_process_f16, ctcbeam::launch_process_bf16)(p, workspace, stream));
 }
 
 int ctcbeam_top_logits(const ctcbeam_rows* logits, int k, float temperature, float* values, int32_t* ids, float* tail,
@@ -216,7 +238,7 @@ int ctcbeam_top_logits(const ctcbeam_rows* logits, int k, float temperature, flo
   p.values = values;
   p.ids = ids;
   p.tail = tail;
-  return launched(ctcbeam::launch_top(p, workspace, stream));
+  return launched(by_type(p.in.type, ctcbeam::launch_top_f32, ctcbeam::launch_top_f16, ctcbeam::launch_top_bf16)(p, workspace, stream));
 }
 
 int ctcbeam_distill(const ctcbeam_rows* student, const float* top_values, const int32_t* top_ids, const float* tail, int k,
@@ -278,7 +300,7 @@ int ctcbeam_distill(const ctcbeam_rows* student, const float* top_values, const 
   p.grad = grad;
   p.grad_stride_b = grad_stride_b;
   p.grad_stride_t = grad_stride_t;
-  return launched(ctcbeam::launch_distill(p, workspace, stream));
+  return launched(by_type(p.in.type, ctcbeam::launch_distill_f32, ctcbeam::launch_distill_f16, ctcbeam::launch_distill_bf16)(p, workspace, stream));
 }
 
 }  // extern "C"

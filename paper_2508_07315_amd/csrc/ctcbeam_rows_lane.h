@@ -6,11 +6,11 @@
 
 #include "ctcbeam_lane.h"
 #include "ctcbeam_rows.h"
+#include "ctcbeam_rows_plan.h"
 
 namespace ctcbeam {
 namespace rows {
 
-constexpr int kThreads = 256;  // per workgroup
 constexpr float kNegInf = -__builtin_huge_valf();
 constexpr float kLargest = 3.402823466e38f;
 constexpr float kLog2e = 1.4426950408889634f;
@@ -211,30 +211,6 @@ struct Layout {
       if (left_label(j) < W) f(F + j, left_label(j));
     }
   }
-  // x[0 .. F+kVec): the row's scores as fp32; `fill` where there is no label
-  __device__ __forceinline__ void load(const T* row, float* x, float fill) const {
-    Bytes16 raw[kVecs];
-    T one[kVec];
-#pragma unroll
-    for (int i = 0; i < kVecs; ++i)
-      if (i < vecs) raw[i] = *reinterpret_cast<const Bytes16*>(row + vec_label(i));
-#pragma unroll
-    for (int j = 0; j < kVec; ++j) {
-      if (j >= left) break;
-      if (left_label(j) < W) one[j] = row[left_label(j)];
-    }
-#pragma unroll
-    for (int i = 0; i < kVecs; ++i) {
-      if (i < vecs) {
-        unpack(raw[i], x + i * kVec, T());
-      } else {
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) x[i * kVec + e] = fill;
-      }
-    }
-#pragma unroll
-    for (int j = 0; j < kVec; ++j) x[F + j] = j < left && left_label(j) < W ? to_float(one[j]) : fill;
-  }
 };
 
 // A row as it was read; each pass over it unpacks it again.
@@ -243,7 +219,9 @@ struct RawRow {
   using L = Layout<T, N, F>;
   Bytes16 raw[L::kVecs] = {};
   T one[L::kVec] = {};
-  __device__ __forceinline__ RawRow(const L& lay, const T* row) {
+  RawRow() = default;
+  __device__ __forceinline__ RawRow(const L& lay, const T* row) { load(lay, row); }
+  __device__ __forceinline__ void load(const L& lay, const T* row) {
 #pragma unroll
     for (int i = 0; i < L::kVecs; ++i)
       if (i < lay.vecs) raw[i] = *reinterpret_cast<const Bytes16*>(row + lay.vec_label(i));
@@ -277,6 +255,17 @@ struct RawRow {
     every(lay, [&](float v, int label, bool there) {
       if (there) f(v, label);
     });
+  }
+  // x[0 .. F+kVec): the values as fp32, as Layout::each counts them
+  __device__ __forceinline__ void values(const L& lay, float* x) const {
+#pragma unroll
+    for (int i = 0; i < L::kVecs; ++i)
+      if (i < lay.vecs) unpack(raw[i], x + i * L::kVec, T());
+#pragma unroll
+    for (int j = 0; j < L::kVec; ++j) {
+      if (j >= lay.left) break;
+      x[L::kVecs * L::kVec + j] = to_float(one[j]);
+    }
   }
   // the largest value, where no value is NaN
   __device__ __forceinline__ float largest(const L& lay) const {
@@ -344,11 +333,6 @@ __device__ __forceinline__ int length_of(const RowsView& v, int b) {
   return l < 0 ? 0 : (l > v.T ? v.T : l);
 }
 
-// A maximum and a sum of exp2((x - max) * log2 e) of parts of a row, as the
-// parts leave them in a workspace.
-struct Part {
-  float m, s;
-};
 __device__ __forceinline__ Part join_parts(const Part* parts, int n) {
   const int lane = threadIdx.x & 63;
   float m = kNegInf, s = 0.0f;

@@ -1,0 +1,122 @@
+// How the row operators cut their work: which kernel takes a call, how many
+// threads a row gets, and whether rows are cut into spans.  Host code, shared by
+// the launches and the workspace sizes.
+//
+// A kernel of N threads and `vecs` vectors of 16 bytes a thread holds rows of
+// fewer than N * (vecs + 1) * (labels of a vector) labels.
+#pragma once
+
+#include <algorithm>
+
+#include "ctcbeam_rows.h"
+
+namespace ctcbeam {
+namespace rows {
+
+constexpr int kThreads = 256;  // per workgroup, but for the rows of more threads
+
+struct ProcessPlan {
+  int spans;   // per row
+  int span;    // labels of a span (the last one may hold fewer)
+  int frames;  // per workgroup
+  int groups;  // of frames, per utterance
+};
+
+// Labels from which on a wave, and a workgroup of 256, do not hold a row of any
+// type in registers as fp32.
+constexpr int kRowOfWave = 64 * 36, kRowOfGroup = 256 * 36;
+
+inline ProcessPlan plan_process(int B, int T, int W, int H, bool normalize, int* n, int* f) {
+  const int64_t rows = static_cast<int64_t>(B) * T;
+  ProcessPlan q{1, W, 1, T};
+  if (W < kRowOfWave && rows >= 1024 && T >= 4) {
+    *n = 64;
+    *f = W < 64 * 20 ? 16 : 32;
+    q.frames = 4;
+  } else if (W < kRowOfGroup && (normalize || rows >= 512)) {
+    *n = 256;
+    *f = W < 256 * 12 ? 8 : W < 256 * 20 ? 16 : 32;
+  } else {
+    // spans: as long as the card stays full of them
+    int span = 8192;
+    while (span > 2048 && rows * ((W + span - 1) / span) < 512) span >>= 1;
+    *n = 256;
+    *f = span / 256;
+    q.spans = (W + span - 1) / span;
+    q.span = span;
+  }
+  // A workgroup's counts serve several frames where the history is longer than
+  // a row and there are workgroups enough (else one frame a wave keeps more
+  // rows in flight: B=64 T=400 W=1025 takes 45 us, with three frames 50).
+  const int64_t groups = rows * q.spans / q.frames;
+  const int more = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({16, groups / 2048, H / W})));
+  q.frames = std::min(q.frames * more, T);
+  q.groups = (T + q.frames - 1) / q.frames;
+  return q;
+}
+
+struct TopPlan {
+  int n, vecs;  // threads of a row (of a span), vectors of 16 bytes of a thread
+  int spans;    // per row
+  int span;     // labels of a span (the last one may hold fewer)
+};
+
+// A wave for each of many short rows; 256 threads for short rows; for longer
+// ones the fewest threads that hold the row where there are rows for every
+// compute unit (1024 rows of 32768: 26 us, of 1024 threads each 31), else 1024
+// (1 row of 32768: 7.6 us, of 256 threads 13.6).
+inline TopPlan plan_top(int type, int B, int T, int W, int k) {
+  const int64_t rows = static_cast<int64_t>(B) * T;
+  const int vec = type == kTypeF32 ? 4 : 8;
+  // threads and their vectors, by what they hold: N * (vecs + 1) * vec - 1 labels
+  const auto holds = [&](int n, int vecs) { return W < n * (vecs + 1) * vec; };
+  if (k <= 32 && rows >= 1024 && W < 64 * 36) return {64, holds(64, 16 / vec) ? 16 / vec : 32 / vec, 1, W};
+  if (holds(256, 4)) return {256, holds(256, 1) ? 1 : holds(256, 2) ? 2 : 4, 1, W};
+  if (rows >= 512) {
+    if (holds(256, 16)) return {256, holds(256, 8) ? 8 : 16, 1, W};
+    if (holds(512, 16)) return {512, 16, 1, W};
+  }
+  if (holds(1024, 16)) return {1024, holds(1024, 4) ? 4 : holds(1024, 8) ? 8 : 16, 1, W};
+  // equal spans of what a workgroup of 1024 holds
+  const int most = 1024 * 17 * vec - 1, spans = (W + most - 1) / most;
+  return {1024, 16, spans, ((W + spans - 1) / spans + 63) / 64 * 64};
+}
+
+struct DistillPlan {
+  int n, f;   // threads of a row (of a span), labels of a thread
+  int spans;  // per row; 0: a workgroup holds the row in packed registers
+  int span;   // labels of a span (the last one may hold fewer)
+};
+
+// A long row keeps the workgroup that holds it busy while few rows leave the
+// card idle; spans use all of it, but read the row twice in two launches.  bf16,
+// k = 64, loss and gradient, us by a workgroup of 1024 a row / by spans:
+//   labels       1 row       128 rows    192 rows    256 rows
+//   18400        7.9 / 9.8   8.9 / 12.5  9.5 / 13.8  9.9 / 14.3
+//   32768        9.9 / 7.9  12.3 / 12.0 13.3 / 14.7 14.6 / 17.5
+//   65536       15.7 / 7.7  19.3 / 16.4 20.2 / 21.1 23.3 / 27.2
+//   131072      27.0 / 7.7  33.3 / 26.7 36.3 / 39.3 39.7 / 47.6
+constexpr int64_t kFewRows = 160;
+constexpr int kLongRow = 24576;
+// Rows from which on smaller workgroups, several of a compute unit, take rows of
+// fewer than 512 * 17 vectors: 512 rows of 18400 by 1024 / 256 threads 27.9 /
+// 30.1 us, 2048 rows 85 / 52 us.
+constexpr int64_t kManyRows = 512;
+
+inline DistillPlan plan_distill(int type, int B, int T, int W) {
+  const int64_t rows = static_cast<int64_t>(B) * T;
+  if (W < 64 * 36 && rows >= 1024) return {64, W < 64 * 20 ? 16 : 32, 1, W};
+  if (W < 256 * 36) return {256, W < 256 * 12 ? 8 : W < 256 * 20 ? 16 : 32, 1, W};
+  const int vec = type == kTypeF32 ? 4 : 8;
+  const auto holds = [&](int n, int vecs) { return W < n * (vecs + 1) * vec; };
+  if ((rows >= kFewRows || W < kLongRow) && holds(1024, 16)) {
+    if (rows >= kManyRows && holds(512, 16)) return {holds(256, 16) ? 256 : 512, (holds(256, 8) ? 8 : 16) * vec, 0, W};
+    return {1024, (holds(1024, 4) ? 4 : holds(1024, 8) ? 8 : 16) * vec, 0, W};
+  }
+  int span = 8192;
+  while (span > 2048 && rows * ((W + span - 1) / span) < 512) span >>= 1;
+  return {256, span / 256, (W + span - 1) / span, span};
+}
+
+}  // namespace rows
+}  // namespace ctcbeam

@@ -12,18 +12,13 @@
 // What bounds it is reading the row.  A wave takes rows of fewer than 2304
 // labels (lists of up to 32), a workgroup longer ones; rows beyond a workgroup
 // are cut into spans whose lists and sums a second launch joins.
-#include <algorithm>
+#pragma once
 
 #include "ctcbeam_rows_lane.h"
+#include "ctcbeam_rows_plan.h"
 
 namespace ctcbeam {
 namespace rows {
-
-struct TopPlan {
-  int n, vecs;  // threads of a row (of a span), vectors of 16 bytes of a thread
-  int spans;    // per row
-  int span;     // labels of a span (the last one may hold fewer)
-};
 
 // what a span leaves for the second launch: k keys, descending (0: none), and
 // the sum over the labels that are not among them
@@ -320,7 +315,7 @@ top_kernel(const TopParams p, const TopPlan plan, void* ws) {
 
 // The lists and sums of a row's spans, joined: a key's place is its place in
 // its own list plus the larger keys of the others, which are in order.
-__global__ void __launch_bounds__(kThreads) join_top_kernel(const TopParams p, const TopPlan plan, const void* ws) {
+static __global__ void __launch_bounds__(kThreads) join_top_kernel(const TopParams p, const TopPlan plan, const void* ws) {
   extern __shared__ uint64_t lists[];  // [spans][k]
   __shared__ float red[4][kThreads / 64];
   const int tid = threadIdx.x, k = p.k, n = plan.spans * k;
@@ -383,23 +378,6 @@ __global__ void __launch_bounds__(kThreads) join_top_kernel(const TopParams p, c
   if (tid == 0) p.tail[row] = s > 0.0f ? m * p.scale + logf(s) : kNegInf;
 }
 
-static TopPlan plan_top(int type, int B, int T, int W, int k) {
-  const int64_t rows = static_cast<int64_t>(B) * T;
-  const int vec = type == kTypeF32 ? 4 : 8;
-  // threads and their vectors, by what they hold: N * (vecs + 1) * vec - 1 labels
-  const auto holds = [&](int n, int vecs) { return W < n * (vecs + 1) * vec; };
-  if (k <= 32 && rows >= 1024 && W < 64 * 36) return {64, holds(64, 16 / vec) ? 16 / vec : 32 / vec, 1, W};
-  if (holds(256, 4)) return {256, holds(256, 1) ? 1 : holds(256, 2) ? 2 : 4, 1, W};
-  if (rows >= 512) {
-    if (holds(256, 16)) return {256, holds(256, 8) ? 8 : 16, 1, W};
-    if (holds(512, 16)) return {512, 16, 1, W};
-  }
-  if (holds(1024, 16)) return {1024, holds(1024, 4) ? 4 : holds(1024, 8) ? 8 : 16, 1, W};
-  // equal spans of what a workgroup of 1024 holds
-  const int most = 1024 * 17 * vec - 1, spans = (W + most - 1) / most;
-  return {1024, 16, spans, ((W + spans - 1) / spans + 63) / 64 * 64};
-}
-
 template <typename T, int N, int VECS>
 static void run_top(const TopParams& p, const TopPlan& q, void* ws, hipStream_t stream) {
   constexpr int threads = N > kThreads ? N : kThreads;
@@ -416,7 +394,7 @@ static void run_top(const TopParams& p, const TopPlan& q, void* ws, hipStream_t 
 }
 
 template <typename T>
-static hipError_t choose_top(const TopParams& p, void* ws, hipStream_t stream) {
+static hipError_t launch_top_impl(const TopParams& p, void* ws, hipStream_t stream) {
   constexpr int V = Packed<T>::kVec;
   const TopPlan q = plan_top(p.in.type, p.in.B, p.in.T, p.in.W, p.k);
   if (q.n == 64) q.vecs == 16 / V ? run_top<T, 64, 16 / V>(p, q, ws, stream) : run_top<T, 64, 32 / V>(p, q, ws, stream);
@@ -436,21 +414,4 @@ static hipError_t choose_top(const TopParams& p, void* ws, hipStream_t stream) {
 }
 
 }  // namespace rows
-
-// (for either width of the scores, as the caller need not say it)
-size_t top_workspace(int B, int T, int W, int k) {
-  size_t most = 0;
-  for (int type : {kTypeF32, kTypeBF16}) {
-    const rows::TopPlan q = rows::plan_top(type, B, T, W, k);
-    if (q.spans > 1) most = std::max(most, static_cast<size_t>(B) * T * q.spans * (k + 1) * sizeof(uint64_t));
-  }
-  return most;
-}
-
-hipError_t launch_top(const TopParams& p, void* workspace, hipStream_t stream) {
-  if (p.in.type == kTypeF32) return rows::choose_top<float>(p, workspace, stream);
-  if (p.in.type == kTypeF16) return rows::choose_top<rows::F16>(p, workspace, stream);
-  return rows::choose_top<rows::BF16>(p, workspace, stream);
-}
-
 }  // namespace ctcbeam

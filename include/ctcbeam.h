@@ -296,7 +296,7 @@ int ctcbeam_query_status(const void* workspace, hipStream_t stream, uint32_t* bi
 #define CTCBEAM_TYPE_BF16 2
 #define CTCBEAM_MAX_LABELS 262144 /* W, labels of a row */
 #define CTCBEAM_MAX_TOP 128       /* k, listed labels of a row */
-#define CTCBEAM_MAX_ROWS 8388608  /* B * T */
+#define CTCBEAM_MAX_ROWS 2097152  /* B * T */
 
 /* Device scores [B, T, W] (for the decoders W = V+1, blank last).  The labels
  * of a row are adjacent; utterances and frames lie stride_b and stride_t

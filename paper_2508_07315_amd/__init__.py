@@ -32,7 +32,7 @@ MAX_V = 4096
 MAX_ORDER = 8
 MAX_LABELS = 1 << 18  # CTCBEAM_MAX_LABELS
 MAX_TOP = 128         # CTCBEAM_MAX_TOP
-MAX_ROWS = 1 << 23    # CTCBEAM_MAX_ROWS
+MAX_ROWS = 1 << 21    # CTCBEAM_MAX_ROWS
 
 
 class CtcbeamError(RuntimeError):

@@ -187,7 +187,7 @@ struct Team {
 // labels costs one load more, not a half-empty vector.
 template <typename T, int N, int F>
 struct Layout {
-  static constexpr int kVec = Packed<T>::kVec, kVecs = F / kVec, kSpan = N * F, kMost = N * (F + kVec) - 1;
+  static constexpr int kVec = Packed<T>::kVec, kVecs = F / kVec;
   int W, tid, vecs, base, left;
   __device__ __forceinline__ Layout(int w, int t) : W(w), tid(t) {
     vecs = w / (N * kVec);

@@ -77,8 +77,8 @@ inline TopPlan plan_top(int type, int B, int T, int W, int k) {
     if (holds(512, 16)) return {512, 16, 1, W};
   }
   if (holds(1024, 16)) return {1024, holds(1024, 4) ? 4 : holds(1024, 8) ? 8 : 16, 1, W};
-  // equal spans of what a workgroup of 1024 holds
-  const int most = 1024 * 17 * vec - 1, spans = (W + most - 1) / most;
+  // equal spans, in whole words of 64 labels, of what a workgroup of 1024 holds
+  const int most = 1024 * 17 * vec - 64, spans = (W + most - 1) / most;
   return {1024, 16, spans, ((W + spans - 1) / spans + 63) / 64 * 64};
 }
 

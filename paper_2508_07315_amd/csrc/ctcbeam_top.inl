@@ -72,10 +72,11 @@ __global__ void __launch_bounds__(N > kThreads ? N : kThreads) __attribute__((am
 top_kernel(const TopParams p, const TopPlan plan, void* ws) {
   using L = Layout<T, N, VECS * Packed<T>::kVec>;
   constexpr int V = L::kVec, kTeams = N > kThreads ? 1 : kThreads / N;
-  constexpr int kRoom = N == 64 ? 256 : 1024, kOwn = kRoom / N;
+  constexpr int kRoom = N == 64 ? 256 : 1024;
   static_assert(N > 64 || (VECS + 1) * V <= 64, "a lane's labels as bits");
   __shared__ float red_all[kTeams][4][N / 64];
   __shared__ __align__(16) uint64_t room_all[kTeams][kRoom + 2];
+  __shared__ float beside[N == 64 ? 1 : kRoom];  // exponentials of the labels behind the list, by place
   __shared__ uint32_t maxima[N == 64 ? 1 : 256];
   __shared__ int found_lds;
   __shared__ uint32_t bound_lds;
@@ -273,13 +274,21 @@ top_kernel(const TopParams p, const TopPlan plan, void* ws) {
     }
     if (place == k - 1) last_all[team] = key;
     if (place >= k) {
-      low += exp2_((key_value(key) - t0) * c);
+      // (the places in `room` of a workgroup's labels depend on its waves' order,
+      // those in the list do not: the sum is to be the same every time)
+      const float e = exp2_((key_value(key) - t0) * c);
+      if constexpr (N == 64) low += e;
+      else beside[place] = e;
     } else if (PART) {
       span_keys(ws, row, plan.spans, span, p.k)[place] = key;
     } else {
       p.values[row * p.k + place] = key_value(key);
       p.ids[row * p.k + place] = key_label(key);
     }
+  }
+  if constexpr (N > 64) {
+    __syncthreads();
+    for (int at = k + tid; at < n; at += N) low += beside[at];
   }
   float ref = t0, s = tm.sum(low);
   if (!(s >= kTooSmall && s < kLargest) && k < lay.W) {

@@ -221,6 +221,15 @@ def test_top_many_rows(W, k, kind):
     top_case(x.to(R.TYPES[kind]).to(dev()), k, [130, 7, 100, 130, 0, 1, 130, 129, 64], 2.0, f"W={W} k={k} {kind}")
 
 
+def test_top_of_the_longest_spans():
+    """A row whose halves, in whole words, are as long as a workgroup holds: the largest labels are the last of each."""
+    W = 139255
+    x = torch.randn((1, 2, W), generator=gen(3))
+    x[..., 69500:69700] += 10.0
+    x[..., -100:] += 10.0
+    top_case(x.to(dev()), 128, what=f"W={W}")
+
+
 def test_top_tail_far_below():
     """What is left may lie far below the list: its log-sum stays finite."""
     x = torch.full((1, 2, 900), -300.0)
@@ -384,6 +393,10 @@ def test_distill_loss_differentiates():
     (P.distill_loss(leaf * 0.5, *args).sum() + P.distill_loss(leaf * 0.5, *args).sum()).backward()
     _, _, want, tol = R.distill(x * 0.5, v, ids, tail, lengths, 2.0)
     R.near(leaf.grad, want, R.rounded_bound(want, tol, "fp32") * 2)
+    leaf = x.clone().requires_grad_()
+    P.distill_loss(leaf, args[0], args[1]).sum().backward()                       # no tail, no lengths
+    _, _, want, tol = R.distill(x, v, ids)
+    R.near(leaf.grad, want, R.rounded_bound(want, tol, "fp32"))
     with torch.no_grad():
         assert not P.distill_loss(leaf, *args).requires_grad
     with pytest.raises(RuntimeError, match="once_differentiable|twice"):
@@ -497,6 +510,31 @@ def test_graphs(B, T, W):
         graphs[i % 2].replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip([o for _, outs in ops for o in outs], want)), f"replay {i}"
+
+
+def test_top_tail_is_the_same_every_time():
+    """Many labels above the bound, found by many waves in any order."""
+    for W, k in ((9000, 128), (60000, 128), (60000, 64), (200000, 100)):
+        x = scores(2, 3, W, "bf16", W)
+        first = P.top_logits(x, k)
+        for _ in range(20):
+            assert all(torch.equal(a, b) for a, b in zip(P.top_logits(x, k), first))
+
+
+def test_distill_loss_is_not_captured():
+    x = scores(1, 2, 40, "fp32", 1).requires_grad_()
+    v, ids, tail = (a.to(dev()) for a in teacher(1, 2, 40, 4, 1))
+    P.distill_loss(x, v, ids, tail)
+    torch.cuda.synchronize()
+    y, g = torch.zeros(4, device=dev()), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        y += 1
+        with pytest.raises(RuntimeError, match="not captured"):
+            P.distill_loss(x, v, ids, tail)
+        loss = P.distill_loss(x.detach(), v, ids, tail)
+    g.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(loss, P.distill_loss(x.detach(), v, ids, tail))
 
 
 def test_same_call_same_bits():

@@ -43,7 +43,7 @@ CALLS = {"process": process, "top": top, "distill": distill}
     (1, "B and T", dict(T=-1)),
     (1, "W must", dict(W=0)),
     (2, "MAX_LABELS", dict(W=P.MAX_LABELS + 1)),
-    (2, "MAX_ROWS", dict(B=1 << 12, T=(1 << 11) + 1)),
+    (2, "MAX_ROWS", dict(B=1 << 10, T=(1 << 11) + 1)),
     (2, "MAX_ROWS", dict(B=(1 << 31) - 1, T=(1 << 31) - 1)),
     (1, "strides", dict(sb=-1)),
     (1, "strides", dict(st=-10)),
@@ -174,3 +174,32 @@ def test_python_wants_device_tensors():
             call()
     with pytest.raises(ValueError, match="constant"):
         P.distill_loss(x, v.requires_grad_(), i)
+
+
+# a row of the most labels, which every operator cuts into spans: they need a workspace
+LONG = dict(B=1, T=1, W=P.MAX_LABELS, sb=P.MAX_LABELS, st=P.MAX_LABELS)
+
+
+@pytest.mark.parametrize("op,need,far", [
+    ("process", lambda lib: lib.ctcbeam_process_workspace_bytes(1, 1, P.MAX_LABELS), dict(out=64 * A)),
+    ("top", lambda lib: lib.ctcbeam_top_workspace_bytes(1, 1, P.MAX_LABELS, 2), {}),
+    ("distill", lambda lib: lib.ctcbeam_distill_workspace_bytes(1, 1, P.MAX_LABELS), dict(grad=64 * A, gsb=P.MAX_LABELS, gst=P.MAX_LABELS)),
+])
+def test_workspace(op, need, far):
+    lib = P._load()
+    n = need(lib)
+    assert n > 0
+    for ws, wn, message in ((None, 0, "too small"), (None, n, "too small"), (48 * A, n - 1, "too small"),
+                            (48 * A + 8, n, "aligned to 16"), (A + 64, n, "overlaps"), (64 * A if op != "top" else 8 * A, n, "overlaps")):
+        assert CALLS[op](rows(**LONG), ws=ws, wn=wn, **far) == 1
+        assert message in lib.ctcbeam_last_error().decode()
+
+
+def test_workspace_of_nothing():
+    lib = P._load()
+    for B, T, W in ((0, 4, 100000), (4, 0, 100000), (-1, 4, 9), (4, 4, 0), (1, 1, P.MAX_LABELS + 1), (1 << 16, 1 << 16, 100000)):
+        assert lib.ctcbeam_process_workspace_bytes(B, T, W) == 0
+        assert lib.ctcbeam_top_workspace_bytes(B, T, W, 4) == 0
+        assert lib.ctcbeam_distill_workspace_bytes(B, T, W) == 0
+    assert lib.ctcbeam_top_workspace_bytes(1, 1, 262144, 0) == 0
+    assert lib.ctcbeam_top_workspace_bytes(1, 1, 262144, 129) == 0

@@ -5,7 +5,9 @@ This module is a thin ctypes binding over the C ABI declared in
 ``include/ctcbeam.h`` and implemented by ``libctcbeam.so`` (host builders in
 ``csrc/ctcbeam_host.cpp``, gfx950 kernels in ``csrc/ctcbeam_decode.inl`` and
 ``csrc/ctcbeam_greedy.inl``, compiled per vocabulary class by the
-``csrc/*.hip`` units).  It only marshals arguments: every step of the search
+``csrc/*.hip`` units; the operators on rows of scores in
+``csrc/ctcbeam_rows_host.cpp``, ``csrc/ctcbeam_process.inl``,
+``csrc/ctcbeam_top.inl`` and ``csrc/ctcbeam_distill.inl``).  It only marshals arguments: every step of the search
 runs in the HIP kernels.  PyTorch supplies device memory and streams; each
 call runs with the inputs' device current, and tensors the binding allocates
 are recorded on the launch stream when it is not torch's current stream.

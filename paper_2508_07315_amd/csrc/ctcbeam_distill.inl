@@ -14,13 +14,22 @@
 // nothing of the list, R is a sum of its own at its own scale, never S less the
 // listed labels, and neither the loss nor the gradient cancels.
 //
-// What bounds it is memory, the row in and the gradient out, and for 16-bit
-// rows nearly as much the exponentials and conversions.  A wave takes rows of
-// fewer than 2304 labels where there are many, a workgroup of 256 rows of
-// fewer than 9216, through a copy of the row in LDS in which the list is taken
-// out and put back.  Longer rows are held by a workgroup of 1024, in packed
-// registers, with a bit per label in LDS; or, where they are few or longer than
-// that, cut into spans whose sums a second launch joins.
+// What bounds it is memory, the row in and the gradient out, and for 16-bit rows
+// nearly as much the exponentials and conversions: 19200 of 25600 rows of 1025
+// bf16 labels, k = 16, take 24 us for 92 MB, 3.8 TB/s (a table of the list's
+// probabilities beside the row, read in both passes, took 34 us); fp32 rows of
+// that length 4.5 TB/s, a copy 5.2.
+//
+// A wave takes rows of fewer than 2304 labels where there are many, a workgroup of
+// 256 rows of fewer than 9216, through a copy of the row in LDS in which the
+// list is taken out and put back.  Longer rows are held by a workgroup of 256 to
+// 1024, in packed registers, with a bit per label in LDS; or, where they are few
+// or longer than that, cut into spans whose sums a second launch joins.  2048
+// rows of 131072 bf16 labels, k = 64: 276 us for 1.07 GB, 3.9 TB/s; in spans
+// 345 us.
+//
+// Scores, sums and probabilities are fp32; a gradient is rounded once, to the
+// student's type.
 #pragma once
 
 #include "ctcbeam_rows_lane.h"

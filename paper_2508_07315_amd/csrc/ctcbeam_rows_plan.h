@@ -29,7 +29,10 @@ constexpr int kRowOfWave = 64 * 36, kRowOfGroup = 256 * 36;
 inline ProcessPlan plan_process(int B, int T, int W, int H, bool normalize, int* n, int* f) {
   const int64_t rows = static_cast<int64_t>(B) * T;
   ProcessPlan q{1, W, 1, T};
-  if (W < kRowOfWave && rows >= 1024 && T >= 4) {
+  if (W < kRowOfWave && rows >= 1024) {
+    // a wave a row, also where an utterance has fewer frames than a workgroup
+    // waves: 4096 requests, T = 1, bf16, us by waves / by workgroups: 33 labels
+    // 6.0 / 9.1, 1025 8.6 / 13.4, 2000 12.8 / 16.0
     *n = 64;
     *f = W < 64 * 20 ? 16 : 32;
     q.frames = 4;
@@ -63,8 +66,9 @@ struct TopPlan {
 
 // A wave for each of many short rows; 256 threads for short rows; for longer
 // ones the fewest threads that hold the row where there are rows for every
-// compute unit (1024 rows of 32768: 26 us, of 1024 threads each 31), else 1024
-// (1 row of 32768: 7.6 us, of 256 threads 13.6).
+// compute unit, else 1024.  bf16, k = 64, us by the fewest / by 1024 threads: 1 row of
+// 32768 labels 13.6 / 7.6; 512 rows 18.7 / 18.2, 1024 rows 25.8 / 34.1, 2048 rows
+// 41 / 63; 2048 rows of 65536 72 / 100.
 inline TopPlan plan_top(int type, int B, int T, int W, int k) {
   const int64_t rows = static_cast<int64_t>(B) * T;
   const int vec = type == kTypeF32 ? 4 : 8;
@@ -99,8 +103,9 @@ struct DistillPlan {
 constexpr int64_t kFewRows = 160;
 constexpr int kLongRow = 24576;
 // Rows from which on smaller workgroups, several of a compute unit, take rows of
-// fewer than 512 * 17 vectors: 512 rows of 18400 by 1024 / 256 threads 27.9 /
-// 30.1 us, 2048 rows 85 / 52 us.
+// fewer than 512 * 17 vectors, us by them / by 1024 threads: 18400 labels, 512 rows
+// 17.7 / 18.9, 2048 rows 40 / 64; 65536 labels, 512 rows 38 / 43,
+// 2048 rows 131 / 171.
 constexpr int64_t kManyRows = 512;
 
 inline DistillPlan plan_distill(int type, int B, int T, int W) {

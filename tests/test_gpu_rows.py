@@ -102,7 +102,7 @@ def test_process_widths(i, W, kind):
 
 
 @pytest.mark.parametrize("B,T,W,H", [(1, 1, 1025, 24), (37, 1, 1025, 9), (5, 1, 32003, 20000), (1, 1, 131072, 1), (9, 130, 33, 5),
-                                     (2, 700, 100, 64), (300, 1, 515, 3)])
+                                     (2, 700, 100, 64), (300, 1, 515, 3), (1100, 1, 1025, 6), (700, 3, 65, 2)])
 def test_process_steps_and_utterances(B, T, W, H):
     process_case(B, T, W, "bf16", B + W, H=H, bias="row", mask="row")
 

@@ -28,6 +28,7 @@ import numpy as np
 _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libctcbeam.so")
 _lib = None
+_torch = None         # the module, once the library is loaded
 
 MAX_K = 128           # CTCBEAM_MAX_K (beams above 64 need V <= 1024)
 MAX_V = 4096
@@ -48,7 +49,7 @@ def library_path() -> str:
 
 
 def _load():
-    global _lib
+    global _lib, _torch
     if _lib is not None:
         return _lib
     if not os.path.exists(LIB_PATH):
@@ -58,7 +59,8 @@ def _load():
     # torch first: its HIP runtime and the system one share a SONAME, so the
     # first loaded serves the whole process; it must be the one that owns
     # torch's device memory and streams
-    import torch  # noqa: F401
+    import torch
+    _torch = torch
     lib = ctypes.CDLL(LIB_PATH)
     P = ctypes.c_void_p
     I = ctypes.c_int
@@ -555,8 +557,7 @@ _TYPES = {}   # CTCBEAM_TYPE_* by torch's type
 
 
 def _need(t, dtype, name, dev):
-    import torch
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+    if not isinstance(t, _torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a device tensor")
     if t.device != dev:
         raise ValueError(f"{name} is on {t.device}, the inputs on {dev}")
@@ -578,10 +579,9 @@ def _pointer(t, dtype, name, shape, dev):
 
 def _rows_of(x, lengths, name):
     """(ctcbeam_rows, B, T, W, device) of scores [B, T, W] with adjacent labels."""
-    import torch
     _need(x, None, name, getattr(x, "device", None))
     if not _TYPES:
-        _TYPES.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2})
+        _TYPES.update({_torch.float32: 0, _torch.float16: 1, _torch.bfloat16: 2})
     code = _TYPES.get(x.dtype)
     if code is None:
         raise TypeError(f"{name} must be float32, float16 or bfloat16, got {x.dtype}")
@@ -593,7 +593,7 @@ def _rows_of(x, lengths, name):
         raise ValueError(f"the labels of a row of {name} must be adjacent")
     dev = x.device
     return _Rows(x.data_ptr(), code, B, T, W, sb, st,
-                 _pointer(lengths, torch.int32, "lengths", (B,), dev)), B, T, W, dev
+                 _pointer(lengths, _torch.int32, "lengths", (B,), dev)), B, T, W, dev
 
 
 def _output(t, dtype, name, shape, like, owned):
@@ -607,14 +607,13 @@ def _output(t, dtype, name, shape, like, owned):
 
 def _workspace(workspace, need, dev, owned):
     """(tensor or None, address, bytes): the given workspace, or one of ``need`` bytes."""
-    import torch
     if workspace is None:
         if not need:
             return None, None, 0
-        workspace = torch.empty((need,), dtype=torch.uint8, device=dev)
+        workspace = _torch.empty((need,), dtype=_torch.uint8, device=dev)
         owned.append(workspace)
         return workspace, workspace.data_ptr(), need
-    return workspace, _dptr(workspace, torch.uint8, "workspace", None, dev), workspace.numel()
+    return workspace, _dptr(workspace, _torch.uint8, "workspace", None, dev), workspace.numel()
 
 
 def ctcbeam_process_logits(logits, lengths=None, history=None, history_lengths=None, penalties=None,
@@ -635,14 +634,13 @@ def ctcbeam_process_logits(logits, lengths=None, history=None, history_lengths=N
     utterance's length are left as they were in ``out``, which may be the
     logits themselves where those are contiguous float32.  No gradient flows
     through this call.  Returns (float32 [B, T, W], workspace or None)."""
-    import torch
     lib = _load()
     rows, B, T, W, dev = _rows_of(logits, lengths, "logits")
     owned = []
-    out, op = _output(out, torch.float32, "out", (B, T, W), logits, owned)
+    out, op = _output(out, _torch.float32, "out", (B, T, W), logits, owned)
     o = _ProcessOpts(repetition=repetition, presence=presence, frequency=frequency, normalize=bool(normalize))
     if history is not None:
-        _need(history, torch.int32, "history", dev)
+        _need(history, _torch.int32, "history", dev)
         if history.dim() != 2 or history.shape[0] != B:
             raise ValueError(f"history must be [{B}, H], got {tuple(history.shape)}")
         H = history.shape[1]
@@ -650,20 +648,20 @@ def ctcbeam_process_logits(logits, lengths=None, history=None, history_lengths=N
             raise ValueError("the tokens of a row of history must be adjacent")
         if H:
             o.history, o.history_size, o.history_stride = history.data_ptr(), H, history.stride(0)
-            o.history_lengths = _pointer(history_lengths, torch.int32, "history_lengths", (B,), dev)
+            o.history_lengths = _pointer(history_lengths, _torch.int32, "history_lengths", (B,), dev)
     elif history_lengths is not None:
         raise ValueError("history_lengths without history")
     if penalties is not None:
-        o.penalties = _pointer(penalties, torch.float32, "penalties", (B, 3), dev)
+        o.penalties = _pointer(penalties, _torch.float32, "penalties", (B, 3), dev)
     if bias is not None:
-        _need(bias, torch.float32, "bias", dev)
+        _need(bias, _torch.float32, "bias", dev)
         if bias.shape != (W,) and bias.shape != (B, W):
             raise ValueError(f"bias must be [{W}] or [{B}, {W}], got {tuple(bias.shape)}")
         if W > 1 and bias.stride(-1) != 1:
             raise ValueError("the labels of a row of bias must be adjacent")
         o.bias, o.bias_stride = bias.data_ptr(), 0 if bias.dim() == 1 else bias.stride(0)
     if mask is not None:
-        _need(mask, torch.int32, "mask", dev)
+        _need(mask, _torch.int32, "mask", dev)
         words = (W + 31) // 32
         if mask.shape != (words,) and mask.shape != (B, words) and mask.shape != (B, T, words):
             raise ValueError(f"mask must be [{words}], [{B}, {words}] or [{B}, {T}, {words}], got {tuple(mask.shape)}")
@@ -686,15 +684,14 @@ def ctcbeam_top_logits(logits, k: int, lengths=None, temperature: float = 1.0, v
     are not listed.  Equal values: the lowest label first; frames behind an
     utterance's length get -inf, -1 and -inf.  No gradient flows through this
     call."""
-    import torch
     lib = _load()
     rows, B, T, W, dev = _rows_of(logits, lengths, "logits")
     k = int(k)
     owned = []
     kk = max(k, 0)
-    values, vp = _output(values, torch.float32, "values", (B, T, kk), logits, owned)
-    ids, ip = _output(ids, torch.int32, "ids", (B, T, kk), logits, owned)
-    tail, tp = _output(tail, torch.float32, "tail", (B, T), logits, owned)
+    values, vp = _output(values, _torch.float32, "values", (B, T, kk), logits, owned)
+    ids, ip = _output(ids, _torch.int32, "ids", (B, T, kk), logits, owned)
+    tail, tp = _output(tail, _torch.float32, "tail", (B, T), logits, owned)
     workspace, wp, wn = _workspace(workspace, lib.ctcbeam_top_workspace_bytes(B, T, W, k), dev, owned)
     _launch(lambda st: lib.ctcbeam_top_logits(ctypes.byref(rows), k, temperature, vp, ip, tp, wp, wn, st),
             dev, stream, owned)
@@ -713,22 +710,21 @@ def ctcbeam_distill(student, values, ids, tail=None, lengths=None, temperature: 
     ``ctcbeam_top_logits`` gives them (``tail=None``: the list is renormalised).
     ``grad`` may have any utterance and frame strides whose rows do not
     overlap.  Returns (loss or None, grad or None, workspace or None)."""
-    import torch
     lib = _load()
     rows, B, T, W, dev = _rows_of(student, lengths, "student")
     owned = []
-    _need(values, torch.float32, "values", dev)
+    _need(values, _torch.float32, "values", dev)
     if values.dim() != 3:
         raise ValueError("values must be [B, T, k]")
     k = values.shape[2]
-    vp = _pointer(values, torch.float32, "values", (B, T, k), dev)
-    ip = _pointer(ids, torch.int32, "ids", (B, T, k), dev)
-    tp = _pointer(tail, torch.float32, "tail", (B, T), dev)
+    vp = _pointer(values, _torch.float32, "values", (B, T, k), dev)
+    ip = _pointer(ids, _torch.int32, "ids", (B, T, k), dev)
+    tp = _pointer(tail, _torch.float32, "tail", (B, T), dev)
     if ip is None:
         raise TypeError("ids must be a device tensor")
     weight, w, wsb, wst = 1.0, None, 0, 0
-    if isinstance(weights, torch.Tensor):
-        _need(weights, torch.float32, "weights", dev)
+    if isinstance(weights, _torch.Tensor):
+        _need(weights, _torch.float32, "weights", dev)
         if weights.shape != (B, T):
             raise ValueError(f"weights must have shape {(B, T)}, got {tuple(weights.shape)}")
         w, (wsb, wst) = weights.data_ptr(), weights.stride()
@@ -737,7 +733,7 @@ def ctcbeam_distill(student, values, ids, tail=None, lengths=None, temperature: 
     lp = gp = None
     gsb = gst = 0
     if want_loss or loss is not None:
-        loss, lp = _output(loss, torch.float32, "loss", (B, T), student, owned)
+        loss, lp = _output(loss, _torch.float32, "loss", (B, T), student, owned)
     if grad is not None:
         _need(grad, student.dtype, "grad", dev)
         if grad.shape != (B, T, W):

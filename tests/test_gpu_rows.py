@@ -102,7 +102,8 @@ def test_process_widths(i, W, kind):
 
 
 @pytest.mark.parametrize("B,T,W,H", [(1, 1, 1025, 24), (37, 1, 1025, 9), (5, 1, 32003, 20000), (1, 1, 131072, 1), (9, 130, 33, 5),
-                                     (2, 700, 100, 64), (300, 1, 515, 3), (1100, 1, 1025, 6), (700, 3, 65, 2)])
+                                     (2, 700, 100, 64), (300, 1, 515, 3), (1100, 1, 1025, 6), (700, 3, 65, 2),
+                                     (70, 1, 40001, 5), (150, 1, 30003, 3), (2, 80, 30003, 40000)])
 def test_process_steps_and_utterances(B, T, W, H):
     process_case(B, T, W, "bf16", B + W, H=H, bias="row", mask="row")
 
@@ -281,7 +282,7 @@ def test_distill_widths(i, W, kind):
 
 @pytest.mark.parametrize("B,T,W,k", [(1, 1, 262144, 128), (260, 1, 700, 4), (1, 300, 1025, 16), (30, 1, 20001, 50),
                                      (300, 4, 33, 5), (2, 520, 1025, 128), (1030, 1, 2303, 16),
-                                     (130, 1, 9216, 20), (2, 65, 40959, 128), (1, 140, 81921, 64), (128, 1, 139263, 9)])
+                                     (130, 1, 9216, 20), (2, 65, 40959, 128), (1, 140, 81921, 64), (128, 1, 139263, 9), (70, 1, 40001, 16)])
 def test_distill_sizes(B, T, W, k):
     v, ids, tail = teacher(B, T, W, k, W)
     distill_case(scores(B, T, W, "bf16", W + 1), v, ids, tail, what=f"B={B} T={T} W={W}", kind="bf16")

@@ -315,7 +315,7 @@ typedef struct ctcbeam_process_opts {
   const int32_t* history;         /* device [B, history_size] labels emitted before,
                                      rows history_stride apart, or NULL; ids outside
                                      0..W-1 (-1 as padding) are ignored */
-  int history_size;
+  int history_size;               /* up to 2^30 (else 2) */
   int64_t history_stride;
   const int32_t* history_lengths; /* device [B] or NULL (all); clamped */
   const float* penalties;         /* device [B, 3] repetition, presence, frequency of

@@ -149,6 +149,7 @@ int ctcbeam_process_logits(const ctcbeam_rows* logits, const ctcbeam_process_opt
   if (int rc = check_rows(logits, &empty)) return rc;
   const ctcbeam_process_opts& o = opts ? *opts : kNone;
   if (o.history_size < 0) return refuse(1, "history_size must be >= 0");
+  if (o.history_size > (1 << 30)) return refuse(2, "history_size above 2^30");
   if (o.history_stride < 0 || o.bias_stride < 0 || o.mask_stride_b < 0 || o.mask_stride_t < 0)
     return refuse(1, "strides must be >= 0");
   if (!o.penalties) {

@@ -77,6 +77,8 @@ def test_no_rows_is_no_work(op, change):
     (1, "presence", dict(presence=float("nan"))),
     (1, "presence", dict(frequency=float("inf"))),
     (1, "history_size", dict(history_size=-1)),
+    (2, "history_size above", dict(history=2 * A, history_size=(1 << 30) + 1)),
+    (2, "history_size above", dict(history=2 * A, history_size=(1 << 31) - 1)),
     (1, "null history", dict(history_size=4)),
     (1, "strides", dict(history=A, history_size=4, history_stride=-4)),
     (1, "strides", dict(bias=A, bias_stride=-10)),

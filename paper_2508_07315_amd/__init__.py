@@ -126,6 +126,15 @@ def _check(rc: int):
         raise CtcbeamError(rc, _load().ctcbeam_last_error().decode())
 
 
+def _size(n, name):
+    """A size as the library's 32-bit int: ctypes would cut a larger one to
+    its low bits, and the library would not see what it has to refuse."""
+    n = int(n)
+    if not -1 << 31 <= n < 1 << 31:
+        raise CtcbeamError(2, f"{name} = {n} does not fit 32 bits")
+    return n
+
+
 class _Opts(ctypes.Structure):
     _fields_ = [("prune_theta", ctypes.c_float), ("stats", ctypes.c_void_p),
                 ("flags", ctypes.c_int), ("reserved", ctypes.c_int * 3)]
@@ -233,7 +242,7 @@ def ctcbeam_lm_build(arrays: dict, host_only: bool = False) -> LM:
     order, counts, ids_p, pr_p, bo_p, keep = _lm_args(arrays)
     out = ctypes.c_void_p()
     fn = lib.ctcbeam_lm_build_host if host_only else lib.ctcbeam_lm_build
-    _check(fn(order, int(arrays["V"]), counts, ids_p, pr_p, bo_p, ctypes.byref(out)))
+    _check(fn(order, _size(arrays["V"], "V"), counts, ids_p, pr_p, bo_p, ctypes.byref(out)))
     del keep
     return LM(out.value, int(arrays["V"]))
 
@@ -246,7 +255,7 @@ def ctcbeam_lm_build_arpa(path: str, vocab_size: int, host_only: bool = False) -
     lib = _load()
     fn = lib.ctcbeam_lm_build_arpa_host if host_only else lib.ctcbeam_lm_build_arpa
     out = ctypes.c_void_p()
-    _check(fn(path.encode(), int(vocab_size), ctypes.byref(out)))
+    _check(fn(path.encode(), _size(vocab_size, "vocab_size"), ctypes.byref(out)))
     return LM(out.value, int(vocab_size))
 
 
@@ -262,7 +271,7 @@ def ctcbeam_boost_build(vocab_size: int, offsets, tokens, host_only: bool = Fals
         tok = np.zeros(1, dtype=np.int32)
     out = ctypes.c_void_p()
     fn = lib.ctcbeam_boost_build_host if host_only else lib.ctcbeam_boost_build
-    _check(fn(int(vocab_size), int(off.shape[0] - 1), off.ctypes.data_as(ctypes.c_void_p),
+    _check(fn(_size(vocab_size, "vocab_size"), _size(off.shape[0] - 1, "phrases"), off.ctypes.data_as(ctypes.c_void_p),
               tok.ctypes.data_as(ctypes.c_void_p), ctypes.byref(out)))
     return Boost(out.value, int(vocab_size))
 
@@ -304,7 +313,7 @@ def ctcbeam_boost_tables(bt: Boost) -> dict:
 
 
 def ctcbeam_workspace_bytes(B: int, T: int, K: int) -> int:
-    return int(_load().ctcbeam_workspace_bytes(int(B), int(T), int(K)))
+    return int(_load().ctcbeam_workspace_bytes(_size(B, "B"), _size(T, "T"), _size(K, "K")))
 
 
 def _dptr(t, dtype, name, shape=None, device=None):
@@ -327,7 +336,7 @@ def _dptr(t, dtype, name, shape=None, device=None):
 def _shape(logprobs):
     if logprobs.dim() != 3:
         raise ValueError("logprobs must be [B, T, V+1]")
-    B, T, W = (int(x) for x in logprobs.shape)
+    B, T, W = (_size(n, name) for n, name in zip(logprobs.shape, ("B", "T", "V+1")))
     return B, T, W - 1, logprobs.device
 
 
@@ -403,6 +412,7 @@ def ctcbeam_decode_ex(logprobs, lengths, K: int, alpha: float = 0.0, beta: float
     import torch
     lib = _load()
     B, T, V, dev = _shape(logprobs)
+    K = _size(K, "K")
     owned, given = [], [] if stats is None else [stats]
     out_tokens = _alloc(out_tokens, (B, T), torch.int32, "out_tokens", dev, owned, given)
     out_lengths = _alloc(out_lengths, (B,), torch.int32, "out_lengths", dev, owned, given)
@@ -411,7 +421,7 @@ def ctcbeam_decode_ex(logprobs, lengths, K: int, alpha: float = 0.0, beta: float
     o = _opts(theta, stats, B, logsumexp, boost_rollback, row_cache, dev, repeat_score)
     args = (_dptr(logprobs, torch.float32, "logprobs", None, dev),
             _dptr(lengths, torch.int32, "lengths", (B,), dev),
-            B, T, V, int(K), float(alpha), float(beta), float(boost_w), *_handles(lm, boost),
+            B, T, V, K, float(alpha), float(beta), float(boost_w), *_handles(lm, boost),
             _dptr(workspace, torch.uint8, "workspace", None, dev), int(workspace.numel()),
             _dptr(out_tokens, torch.int32, "out_tokens", (B, T), dev),
             _dptr(out_lengths, torch.int32, "out_lengths", (B,), dev),
@@ -445,7 +455,7 @@ def ctcbeam_decode_nbest(logprobs, lengths, K: int, alpha: float = 0.0, beta: fl
     import torch
     lib = _load()
     B, T, V, dev = _shape(logprobs)
-    K = int(K)
+    K = _size(K, "K")
     owned, given = [], [] if stats is None else [stats]
     nbest_tokens = _alloc(nbest_tokens, (B, K, T), torch.int32, "nbest_tokens", dev, owned, given)
     nbest_lengths = _alloc(nbest_lengths, (B, K), torch.int32, "nbest_lengths", dev, owned, given)
@@ -510,6 +520,7 @@ def ctcbeam_decode_noalloc(logprobs, lengths, K: int, alpha: float = 0.0, beta: 
     import torch
     lib = _load()
     B, T, V, dev = _shape(logprobs)
+    K = _size(K, "K")
     owned, given = [], [] if stats is None else [stats]
     out_tokens = _alloc(out_tokens, (B, T), torch.int32, "out_tokens", dev, owned, given)
     out_lengths = _alloc(out_lengths, (B,), torch.int32, "out_lengths", dev, owned, given)
@@ -517,7 +528,7 @@ def ctcbeam_decode_noalloc(logprobs, lengths, K: int, alpha: float = 0.0, beta: 
     o = _opts(theta, stats, B, logsumexp, boost_rollback, row_cache, dev, repeat_score)
     args = (_dptr(logprobs, torch.float32, "logprobs", None, dev),
             _dptr(lengths, torch.int32, "lengths", (B,), dev),
-            B, T, V, int(K), float(alpha), float(beta), float(boost_w), *_handles(lm, boost),
+            B, T, V, K, float(alpha), float(beta), float(boost_w), *_handles(lm, boost),
             _dptr(out_tokens, torch.int32, "out_tokens", (B, T), dev),
             _dptr(out_lengths, torch.int32, "out_lengths", (B,), dev),
             _dptr(out_scores, torch.float32, "out_scores", (B,), dev))
@@ -605,6 +616,8 @@ def _rows_of(x, lengths, name):
     if x.dim() != 3:
         raise ValueError(f"{name} must be [B, T, W]")
     B, T, W = x.shape
+    if max(B, T, W) >= 1 << 31:
+        _size(B, "B"), _size(T, "T"), _size(W, "W")
     sb, st, sl = x.stride()
     if sl != 1 and W > 1:
         raise ValueError(f"the labels of a row of {name} must be adjacent")
@@ -661,7 +674,7 @@ def ctcbeam_process_logits(logits, lengths=None, history=None, history_lengths=N
         _need(history, _torch.int32, "history", dev)
         if history.dim() != 2 or history.shape[0] != B:
             raise ValueError(f"history must be [{B}, H], got {tuple(history.shape)}")
-        H = history.shape[1]
+        H = _size(history.shape[1], "history_size")
         if H > 1 and history.stride(1) != 1:
             raise ValueError("the tokens of a row of history must be adjacent")
         if H:
@@ -704,7 +717,7 @@ def ctcbeam_top_logits(logits, k: int, lengths=None, temperature: float = 1.0, v
     call."""
     lib = _load()
     rows, B, T, W, dev = _rows_of(logits, lengths, "logits")
-    k = int(k)
+    k = _size(k, "k")
     owned, given = [], []
     kk = max(k, 0)
     values, vp = _output(values, _torch.float32, "values", (B, T, kk), logits, owned, given)
@@ -734,7 +747,7 @@ def ctcbeam_distill(student, values, ids, tail=None, lengths=None, temperature: 
     _need(values, _torch.float32, "values", dev)
     if values.dim() != 3:
         raise ValueError("values must be [B, T, k]")
-    k = values.shape[2]
+    k = _size(values.shape[2], "k")
     vp = _pointer(values, _torch.float32, "values", (B, T, k), dev)
     ip = _pointer(ids, _torch.int32, "ids", (B, T, k), dev)
     tp = _pointer(tail, _torch.float32, "tail", (B, T), dev)

@@ -364,6 +364,8 @@ int ctcbeam_process_logits(const ctcbeam_rows* logits, const ctcbeam_process_opt
  * -inf where nothing is left.  With the list this is the whole distribution's
  * mass, without the cancellation of 1 - sum p.
  *   k           : 1..min(W, CTCBEAM_MAX_TOP)
+ *   temperature : positive and finite, and so must log2(e)/temperature be as
+ *                 fp32 numbers (from about 4.3e-39 on; else 1)
  *   values, ids : device fp32 / int32 [B, T, k]; tail: device fp32 [B, T].
  *   Frames t >= L_b get values -inf, ids -1 and tail -inf.
  */
@@ -390,6 +392,7 @@ int ctcbeam_top_logits(const ctcbeam_rows* logits, int k, float temperature, flo
  * gives loss +inf and a finite gradient; NaN or +inf in a student row gives
  * NaN.
  *   top_values, top_ids : device [B, T, k], k in 1..CTCBEAM_MAX_TOP
+ *   temperature : as for ctcbeam_top_logits
  *   tail    : device [B, T] or NULL, log-sum at `temperature`
  *   weights : device, weight of row (b, t) at b*weight_stride_b +
  *             t*weight_stride_t, or NULL: `weight`.  Only grad is weighted.

@@ -88,6 +88,11 @@ int check_rows(const ctcbeam_rows* r, bool* empty) {
   return 0;
 }
 
+// (the kernels' exponents are (x - max) * (scale * log2 e): 0 where x is the maximum)
+bool usable(float temperature, float scale) {
+  return temperature > 0.0f && std::isfinite(temperature) && scale > 0.0f && std::isfinite(scale * 1.4426950408889634f);
+}
+
 ctcbeam::RowsView view(const ctcbeam_rows* r) {
   return {r->data, r->lengths, r->stride_b, r->stride_t, r->type, r->B, r->T, r->W};
 }
@@ -213,8 +218,7 @@ int ctcbeam_top_logits(const ctcbeam_rows* logits, int k, float temperature, flo
   if (k > CTCBEAM_MAX_TOP) return refuse(2, "k above CTCBEAM_MAX_TOP");
   if (k > logits->W) return refuse(1, "k above W");
   const float scale = 1.0f / temperature;
-  if (!(temperature > 0.0f) || !std::isfinite(temperature) || !std::isfinite(scale) || !(scale > 0.0f))
-    return refuse(1, "temperature must be positive and finite");
+  if (!usable(temperature, scale)) return refuse(1, "temperature must be positive and finite, and so must log2(e)/temperature");
   if (empty) return 0;
   if (!values || !ids || !tail) return refuse(1, "null output pointer");
   if (misaligned(values, 4) || misaligned(ids, 4) || misaligned(tail, 4))
@@ -251,8 +255,7 @@ int ctcbeam_distill(const ctcbeam_rows* student, const float* top_values, const 
   if (k < 1) return refuse(1, "k must be >= 1");
   if (k > CTCBEAM_MAX_TOP) return refuse(2, "k above CTCBEAM_MAX_TOP");
   const float scale = 1.0f / temperature;
-  if (!(temperature > 0.0f) || !std::isfinite(temperature) || !std::isfinite(scale) || !(scale > 0.0f))
-    return refuse(1, "temperature must be positive and finite");
+  if (!usable(temperature, scale)) return refuse(1, "temperature must be positive and finite, and so must log2(e)/temperature");
   if (!weights && !std::isfinite(weight)) return refuse(1, "weight must be finite");
   if (weight_stride_b < 0 || weight_stride_t < 0 || grad_stride_b < 0 || grad_stride_t < 0)
     return refuse(1, "strides must be >= 0");

@@ -54,10 +54,14 @@ Wide extent(int64_t B, int64_t T, int64_t W, int64_t sb, int64_t st) {
 
 bool meet(const Span& a, const Span& b) { return a.lo < b.hi && b.lo < a.hi; }
 
-bool meet_any(const Span& a, std::initializer_list<Span> others) {
+template <typename Spans>
+bool meet_any(const Span& a, const Spans& others) {
   for (const Span& o : others)
     if (meet(a, o)) return true;
   return false;
+}
+bool meet_any(const Span& a, std::initializer_list<Span> others) {
+  return meet_any<std::initializer_list<Span>>(a, others);
 }
 
 int element_size(int type) { return type == CTCBEAM_TYPE_F32 ? 4 : 2; }
@@ -178,15 +182,16 @@ int ctcbeam_process_logits(const ctcbeam_rows* logits, const ctcbeam_process_opt
   const bool in_place = logits->data == out && logits->type == CTCBEAM_TYPE_F32 &&
                         (T == 1 || logits->stride_t == W) && (B == 1 || logits->stride_b == static_cast<int64_t>(T) * W);
   if (meet(so, si) && !in_place) return refuse(1, "out overlaps the logits (and is not the same contiguous fp32 rows)");
-  if (meet_any(so, {span(logits->lengths, B, 4), span(with_history ? o.history : nullptr, h, 4),
-                    span(o.history_lengths, B, 4), span(o.penalties, 3 * static_cast<Wide>(B), 4), span(o.bias, bi, 4),
-                    span(o.mask, ma, 4)}))
-    return refuse(1, "out overlaps an input");
+  const Span inputs[] = {span(logits->lengths, B, 4),   span(with_history ? o.history : nullptr, h, 4),
+                         span(o.history_lengths, B, 4), span(o.penalties, 3 * static_cast<Wide>(B), 4),
+                         span(o.bias, bi, 4),           span(o.mask, ma, 4)};
+  if (meet_any(so, inputs)) return refuse(1, "out overlaps an input");
   if (workspace_bytes < ctcbeam_process_workspace_bytes(B, T, W) ||
       (!workspace && ctcbeam_process_workspace_bytes(B, T, W) > 0))
     return refuse(1, "workspace too small");
   if (misaligned(workspace, 16)) return refuse(1, "workspace is not aligned to 16 bytes");
-  if (meet_any(span(workspace, static_cast<Wide>(workspace_bytes), 1), {so, si})) return refuse(1, "workspace overlaps another argument");
+  const Span sw = span(workspace, static_cast<Wide>(workspace_bytes), 1);
+  if (meet_any(sw, {so, si}) || meet_any(sw, inputs)) return refuse(1, "workspace overlaps another argument");
   if (int rc = device_there()) return rc;
   ctcbeam::ProcessParams p{};
   p.in = view(logits);

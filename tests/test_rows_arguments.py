@@ -6,7 +6,7 @@ import struct
 import pytest
 
 import paper_2508_07315_amd as P
-from test_rows_refusals import distill, rows, top
+from test_rows_refusals import A, LONG, distill, process, rows, top
 
 
 def message():
@@ -26,3 +26,22 @@ def test_temperature(temperature, good):
     for call in (lambda: top(rows(), temperature=temperature, values=None), lambda: distill(rows(), temperature=temperature, values=None)):
         assert call() == 1
         assert ("null" if good else "temperature") in message()
+
+
+# the longest row's arguments, each with its size in bytes; the row lies at A, its scores at 64 A
+W = P.MAX_LABELS
+INPUTS = dict(lengths=(8 * A, 4), history=(16 * A, 4 * 1000), history_lengths=(17 * A, 4), penalties=(18 * A, 12),
+              bias=(20 * A, 4 * W), mask=(32 * A, W // 8))
+
+
+@pytest.mark.parametrize("name", INPUTS)
+def test_process_workspace_on_an_input(name):
+    """The first launch would write where others, and the second one, still read."""
+    lib = P._load()
+    n = lib.ctcbeam_process_workspace_bytes(1, 1, W)
+    given = {k: v[0] for k, v in INPUTS.items()}
+    lengths = given.pop("lengths")
+    at, size = INPUTS[name]
+    for ws in (at, at + (size - 1) // 16 * 16, at - (n - 1) // 16 * 16):
+        assert process(rows(**LONG, lengths=lengths), out=64 * A, history_size=1000, ws=ws, wn=n, **given) == 1
+        assert message() == "workspace overlaps another argument"

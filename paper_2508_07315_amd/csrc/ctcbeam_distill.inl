@@ -525,7 +525,8 @@ static hipError_t launch_distill_impl(const DistillParams& p, void* workspace, h
     else if (q.n == 1024) distill_wide_kernel<T, 1024, 16><<<rows, 1024, 0, stream>>>(p);
     else if (q.n == 512) distill_wide_kernel<T, 512, 16><<<rows, 512, 0, stream>>>(p);
     else if (vecs == 16) distill_wide_kernel<T, 256, 16><<<rows, 256, 0, stream>>>(p);
-    else distill_wide_kernel<T, 256, 8><<<rows, 256, 0, stream>>>(p);
+    // (8 vectors of fp32 hold rows of fewer than kRowOfGroup labels, which come through LDS)
+    else if constexpr (Packed<T>::kVec == 8) distill_wide_kernel<T, 256, 8><<<rows, 256, 0, stream>>>(p);
   } else if (q.n == 64) q.f == 16 ? run_distill<T, 64, 16>(p, q, sums, stream) : run_distill<T, 64, 32>(p, q, sums, stream);
   else if (q.f == 8) run_distill<T, 256, 8>(p, q, sums, stream);
   else if (q.f == 16) run_distill<T, 256, 16>(p, q, sums, stream);

@@ -13,7 +13,8 @@ HIP = "/opt/rocm/include"
 TYPES = {"fp32": 0, "fp16": 1, "bf16": 2}
 
 # Calls as lines "op type B T W k H normalize" (what an operator does not have
-# is 0), each answered by a line of the kernels it launches; "all" answers with
+# is 0), each answered by a line of the kernels it launches
+# (and of whether a workgroup's count of the history serves frame after frame); "all" answers with
 # the kernels of all sizes.
 PROGRAM = r"""
 #include "ctcbeam_rows_plan.h"
@@ -32,8 +33,9 @@ static std::string of(const std::string& op, int type, int B, int T, int W, int 
   if (op == "process") {
     int n, f;
     const ProcessPlan q = plan_process(B, T, W, H, normalize, &n, &f);
-    if (q.spans > 1 && normalize) return form("process_kernel", type, n, f, ", 1") + form("process_kernel", type, n, f, ", 2");
-    return form("process_kernel", type, n, f, ", 0");
+    const std::string shared = q.frames > kThreads / n ? "counts for several frames, " + std::to_string(n) + (q.spans > 1 ? ", spans;" : ";") : "";
+    if (q.spans > 1 && normalize) return shared + form("process_kernel", type, n, f, ", 1") + form("process_kernel", type, n, f, ", 2");
+    return shared + form("process_kernel", type, n, f, ", 0");
   }
   if (op == "top") {
     const TopPlan q = plan_top(type, B, T, W, k);

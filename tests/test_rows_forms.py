@@ -7,6 +7,7 @@ import subprocess
 import pytest
 
 import paper_2508_07315_amd as P
+import rows_calls
 from rows_forms import Forms
 
 
@@ -30,3 +31,10 @@ def test_compiled_and_reachable_kernels_are_the_same(forms):
     have, reached = compiled(), forms.all()
     assert reached - have == set(), "plans that pick a kernel which is not compiled"
     assert have - reached == set(), "kernels that no call runs"
+
+
+def test_every_kernel_is_run_on_the_gpu(forms):
+    calls = list(rows_calls.every())
+    run = {f for found in forms.of(calls) for f in found}
+    assert forms.all() - run == set()
+    assert {"counts for several frames, 64", "counts for several frames, 256"} <= run

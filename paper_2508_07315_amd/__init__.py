@@ -10,7 +10,8 @@ This module is a thin ctypes binding over the C ABI declared in
 ``csrc/ctcbeam_top.inl`` and ``csrc/ctcbeam_distill.inl``).  It only marshals arguments: every step of the search
 runs in the HIP kernels.  PyTorch supplies device memory and streams; each
 call runs with the inputs' device current, and tensors the binding allocates
-are recorded on the launch stream when it is not torch's current stream.
+are the launch stream's, and recorded on torch's current stream where that is
+another one.
 Outputs that the caller gives count as written in place for torch's autograd,
 and may not require a gradient while torch records one.
 
@@ -341,32 +342,49 @@ def _shape(logprobs):
 
 
 def _stream_handle(stream, dev):
-    """(raw hipStream_t, torch stream object or None) for ``stream``: None
-    (torch's current stream on dev), a torch.cuda.Stream, or a raw handle."""
+    """Raw hipStream_t of ``stream``: None (torch's current stream on dev), a
+    torch.cuda.Stream, or a raw handle."""
     import torch
     if stream is None:
-        return torch.cuda.current_stream(dev).cuda_stream, None
+        return torch.cuda.current_stream(dev).cuda_stream
     if isinstance(stream, torch.cuda.Stream):
-        return stream.cuda_stream, stream
-    return int(stream), None
+        return stream.cuda_stream
+    return int(stream)
+
+
+def _empty(shape, dtype, dev, stream, owned):
+    """A new tensor for a launch on ``stream``, in memory of that stream: what
+    torch's current stream has freed may still be in use by work queued there,
+    which the launch does not wait for."""
+    import torch
+    if stream is None:
+        t = torch.empty(shape, dtype=dtype, device=dev)
+    else:
+        if not isinstance(stream, torch.cuda.Stream):
+            stream = torch.cuda.ExternalStream(int(stream), device=dev)
+        with torch.cuda.stream(stream):
+            t = torch.empty(shape, dtype=dtype, device=dev)
+    owned.append(t)
+    return t
 
 
 def _launch(call, dev, stream, owned, given):
     """Run ``call(raw_stream)`` (one C entry point, returning its code) with
     the inputs' device current.  Tensors the binding allocated (``owned``)
-    are recorded on the launch stream when it is not torch's current stream,
+    are recorded on torch's current stream where that is not the launch stream,
     so the caching allocator does not hand their memory to other work before
-    the kernel is done with it.  The caller's outputs (``given``) count as
+    the caller's is done with it.  The caller's outputs (``given``) count as
     written in place, so that a backward pass that saved one before fails
     instead of reading what is there now."""
     import torch
     with torch.cuda.device(dev):
-        raw, obj = _stream_handle(stream, dev)
+        raw = _stream_handle(stream, dev)
         _check(call(ctypes.c_void_p(raw)))
-        if owned and raw != torch.cuda.current_stream(dev).cuda_stream:
-            rec = obj if obj is not None else torch.cuda.ExternalStream(raw, device=dev)
-            for t in owned:
-                t.record_stream(rec)
+        if owned and stream is not None:
+            current = torch.cuda.current_stream(dev)
+            if raw != current.cuda_stream:
+                for t in owned:
+                    t.record_stream(current)
     if given:
         torch.autograd.graph.increment_version(given)
 
@@ -384,13 +402,10 @@ def _take(t, name, given):
         given.append(t)
 
 
-def _alloc(t, shape, dtype, name, dev, owned, given):
-    import torch
+def _alloc(t, shape, dtype, name, dev, stream, owned, given):
     if t is None:
-        t = torch.empty(shape, dtype=dtype, device=dev)
-        owned.append(t)
-    else:
-        _take(t, name, given)
+        return _empty(shape, dtype, dev, stream, owned)
+    _take(t, name, given)
     return t
 
 
@@ -414,10 +429,10 @@ def ctcbeam_decode_ex(logprobs, lengths, K: int, alpha: float = 0.0, beta: float
     B, T, V, dev = _shape(logprobs)
     K = _size(K, "K")
     owned, given = [], [] if stats is None else [stats]
-    out_tokens = _alloc(out_tokens, (B, T), torch.int32, "out_tokens", dev, owned, given)
-    out_lengths = _alloc(out_lengths, (B,), torch.int32, "out_lengths", dev, owned, given)
-    out_scores = _alloc(out_scores, (B,), torch.float32, "out_scores", dev, owned, given)
-    workspace = _alloc(workspace, (max(ctcbeam_workspace_bytes(B, T, K), 1),), torch.uint8, "workspace", dev, owned, given)
+    out_tokens = _alloc(out_tokens, (B, T), torch.int32, "out_tokens", dev, stream, owned, given)
+    out_lengths = _alloc(out_lengths, (B,), torch.int32, "out_lengths", dev, stream, owned, given)
+    out_scores = _alloc(out_scores, (B,), torch.float32, "out_scores", dev, stream, owned, given)
+    workspace = _alloc(workspace, (max(ctcbeam_workspace_bytes(B, T, K), 1),), torch.uint8, "workspace", dev, stream, owned, given)
     o = _opts(theta, stats, B, logsumexp, boost_rollback, row_cache, dev, repeat_score)
     args = (_dptr(logprobs, torch.float32, "logprobs", None, dev),
             _dptr(lengths, torch.int32, "lengths", (B,), dev),
@@ -457,10 +472,10 @@ def ctcbeam_decode_nbest(logprobs, lengths, K: int, alpha: float = 0.0, beta: fl
     B, T, V, dev = _shape(logprobs)
     K = _size(K, "K")
     owned, given = [], [] if stats is None else [stats]
-    nbest_tokens = _alloc(nbest_tokens, (B, K, T), torch.int32, "nbest_tokens", dev, owned, given)
-    nbest_lengths = _alloc(nbest_lengths, (B, K), torch.int32, "nbest_lengths", dev, owned, given)
-    nbest_scores = _alloc(nbest_scores, (B, K), torch.float32, "nbest_scores", dev, owned, given)
-    workspace = _alloc(workspace, (max(ctcbeam_workspace_bytes(B, T, K), 1),), torch.uint8, "workspace", dev, owned, given)
+    nbest_tokens = _alloc(nbest_tokens, (B, K, T), torch.int32, "nbest_tokens", dev, stream, owned, given)
+    nbest_lengths = _alloc(nbest_lengths, (B, K), torch.int32, "nbest_lengths", dev, stream, owned, given)
+    nbest_scores = _alloc(nbest_scores, (B, K), torch.float32, "nbest_scores", dev, stream, owned, given)
+    workspace = _alloc(workspace, (max(ctcbeam_workspace_bytes(B, T, K), 1),), torch.uint8, "workspace", dev, stream, owned, given)
     o = _opts(theta, stats, B, logsumexp, boost_rollback, row_cache, dev, repeat_score)
     args = (_dptr(logprobs, torch.float32, "logprobs", None, dev),
             _dptr(lengths, torch.int32, "lengths", (B,), dev),
@@ -486,10 +501,10 @@ def ctcbeam_greedy_decode(logprobs, lengths, alpha: float = 0.0, beta: float = 0
     lib = _load()
     B, T, V, dev = _shape(logprobs)
     owned, given = [], [] if stats is None else [stats]
-    out_tokens = _alloc(out_tokens, (B, T), torch.int32, "out_tokens", dev, owned, given)
-    out_lengths = _alloc(out_lengths, (B,), torch.int32, "out_lengths", dev, owned, given)
-    out_scores = _alloc(out_scores, (B,), torch.float32, "out_scores", dev, owned, given)
-    workspace = _alloc(workspace, (max(ctcbeam_workspace_bytes(B, 0, 1), 1),), torch.uint8, "workspace", dev, owned, given)
+    out_tokens = _alloc(out_tokens, (B, T), torch.int32, "out_tokens", dev, stream, owned, given)
+    out_lengths = _alloc(out_lengths, (B,), torch.int32, "out_lengths", dev, stream, owned, given)
+    out_scores = _alloc(out_scores, (B,), torch.float32, "out_scores", dev, stream, owned, given)
+    workspace = _alloc(workspace, (max(ctcbeam_workspace_bytes(B, 0, 1), 1),), torch.uint8, "workspace", dev, stream, owned, given)
     o = _opts(math.inf, stats, B, False, boost_rollback, True, dev, repeat_score)
     args = (_dptr(logprobs, torch.float32, "logprobs", None, dev),
             _dptr(lengths, torch.int32, "lengths", (B,), dev),
@@ -522,9 +537,9 @@ def ctcbeam_decode_noalloc(logprobs, lengths, K: int, alpha: float = 0.0, beta: 
     B, T, V, dev = _shape(logprobs)
     K = _size(K, "K")
     owned, given = [], [] if stats is None else [stats]
-    out_tokens = _alloc(out_tokens, (B, T), torch.int32, "out_tokens", dev, owned, given)
-    out_lengths = _alloc(out_lengths, (B,), torch.int32, "out_lengths", dev, owned, given)
-    out_scores = _alloc(out_scores, (B,), torch.float32, "out_scores", dev, owned, given)
+    out_tokens = _alloc(out_tokens, (B, T), torch.int32, "out_tokens", dev, stream, owned, given)
+    out_lengths = _alloc(out_lengths, (B,), torch.int32, "out_lengths", dev, stream, owned, given)
+    out_scores = _alloc(out_scores, (B,), torch.float32, "out_scores", dev, stream, owned, given)
     o = _opts(theta, stats, B, logsumexp, boost_rollback, row_cache, dev, repeat_score)
     args = (_dptr(logprobs, torch.float32, "logprobs", None, dev),
             _dptr(lengths, torch.int32, "lengths", (B,), dev),
@@ -544,7 +559,7 @@ def ctcbeam_query_status(workspace, stream=None) -> int:
     dev = workspace.device
     bits = ctypes.c_uint32(0)
     with torch.cuda.device(dev):
-        raw, _ = _stream_handle(stream, dev)
+        raw = _stream_handle(stream, dev)
         _check(_load().ctcbeam_query_status(ctypes.c_void_p(workspace.data_ptr()),
                                             ctypes.c_void_p(raw), ctypes.byref(bits)))
     return int(bits.value)
@@ -626,23 +641,21 @@ def _rows_of(x, lengths, name):
                  _pointer(lengths, _torch.int32, "lengths", (B,), dev)), B, T, W, dev
 
 
-def _output(t, dtype, name, shape, like, owned, given):
+def _output(t, dtype, name, shape, dev, stream, owned, given):
     """(tensor, address) of an output: the given one, or a new one."""
     if t is None:
-        t = like.new_empty(shape, dtype=dtype)
-        owned.append(t)
+        t = _empty(shape, dtype, dev, stream, owned)
         return t, t.data_ptr()
     _take(t, name, given)
-    return t, _pointer(t, dtype, name, shape, like.device)
+    return t, _pointer(t, dtype, name, shape, dev)
 
 
-def _workspace(workspace, need, dev, owned):
+def _workspace(workspace, need, dev, stream, owned):
     """(tensor or None, address, bytes): the given workspace, or one of ``need`` bytes."""
     if workspace is None:
         if not need:
             return None, None, 0
-        workspace = _torch.empty((need,), dtype=_torch.uint8, device=dev)
-        owned.append(workspace)
+        workspace = _empty((need,), _torch.uint8, dev, stream, owned)
         return workspace, workspace.data_ptr(), need
     return workspace, _dptr(workspace, _torch.uint8, "workspace", None, dev), workspace.numel()
 
@@ -668,7 +681,7 @@ def ctcbeam_process_logits(logits, lengths=None, history=None, history_lengths=N
     lib = _load()
     rows, B, T, W, dev = _rows_of(logits, lengths, "logits")
     owned, given = [], []
-    out, op = _output(out, _torch.float32, "out", (B, T, W), logits, owned, given)
+    out, op = _output(out, _torch.float32, "out", (B, T, W), dev, stream, owned, given)
     o = _ProcessOpts(repetition=repetition, presence=presence, frequency=frequency, normalize=bool(normalize))
     if history is not None:
         _need(history, _torch.int32, "history", dev)
@@ -701,7 +714,7 @@ def ctcbeam_process_logits(logits, lengths=None, history=None, history_lengths=N
         o.mask = mask.data_ptr()
         o.mask_stride_b = mask.stride(0) if mask.dim() > 1 else 0
         o.mask_stride_t = mask.stride(1) if mask.dim() > 2 else 0
-    workspace, wp, wn = _workspace(workspace, lib.ctcbeam_process_workspace_bytes(B, T, W), dev, owned)
+    workspace, wp, wn = _workspace(workspace, lib.ctcbeam_process_workspace_bytes(B, T, W), dev, stream, owned)
     _launch(lambda st: lib.ctcbeam_process_logits(ctypes.byref(rows), ctypes.byref(o), op, wp, wn, st),
             dev, stream, owned, given)
     return out, workspace
@@ -720,10 +733,10 @@ def ctcbeam_top_logits(logits, k: int, lengths=None, temperature: float = 1.0, v
     k = _size(k, "k")
     owned, given = [], []
     kk = max(k, 0)
-    values, vp = _output(values, _torch.float32, "values", (B, T, kk), logits, owned, given)
-    ids, ip = _output(ids, _torch.int32, "ids", (B, T, kk), logits, owned, given)
-    tail, tp = _output(tail, _torch.float32, "tail", (B, T), logits, owned, given)
-    workspace, wp, wn = _workspace(workspace, lib.ctcbeam_top_workspace_bytes(B, T, W, k), dev, owned)
+    values, vp = _output(values, _torch.float32, "values", (B, T, kk), dev, stream, owned, given)
+    ids, ip = _output(ids, _torch.int32, "ids", (B, T, kk), dev, stream, owned, given)
+    tail, tp = _output(tail, _torch.float32, "tail", (B, T), dev, stream, owned, given)
+    workspace, wp, wn = _workspace(workspace, lib.ctcbeam_top_workspace_bytes(B, T, W, k), dev, stream, owned)
     _launch(lambda st: lib.ctcbeam_top_logits(ctypes.byref(rows), k, temperature, vp, ip, tp, wp, wn, st),
             dev, stream, owned, given)
     return values, ids, tail, workspace
@@ -764,7 +777,7 @@ def ctcbeam_distill(student, values, ids, tail=None, lengths=None, temperature: 
     lp = gp = None
     gsb = gst = 0
     if want_loss or loss is not None:
-        loss, lp = _output(loss, _torch.float32, "loss", (B, T), student, owned, given)
+        loss, lp = _output(loss, _torch.float32, "loss", (B, T), dev, stream, owned, given)
     if grad is not None:
         _need(grad, student.dtype, "grad", dev)
         if grad.shape != (B, T, W):
@@ -775,9 +788,9 @@ def ctcbeam_distill(student, values, ids, tail=None, lengths=None, temperature: 
         _take(grad, "grad", given)
         gp = grad.data_ptr()
     elif want_grad:
-        grad, gp = _output(None, student.dtype, "grad", (B, T, W), student, owned, given)
+        grad, gp = _output(None, student.dtype, "grad", (B, T, W), dev, stream, owned, given)
         gsb, gst = T * W, W
-    workspace, wp, wn = _workspace(workspace, lib.ctcbeam_distill_workspace_bytes(B, T, W), dev, owned)
+    workspace, wp, wn = _workspace(workspace, lib.ctcbeam_distill_workspace_bytes(B, T, W), dev, stream, owned)
     _launch(lambda st: lib.ctcbeam_distill(ctypes.byref(rows), vp, ip, tp, k, temperature, w, wsb, wst, weight,
                                            lp, gp, gsb, gst, wp, wn, st), dev, stream, owned, given)
     return loss, grad, workspace

@@ -344,10 +344,9 @@ def _shape(logprobs):
 def _stream_handle(stream, dev):
     """Raw hipStream_t of ``stream``: None (torch's current stream on dev), a
     torch.cuda.Stream, or a raw handle."""
-    import torch
     if stream is None:
-        return torch.cuda.current_stream(dev).cuda_stream
-    if isinstance(stream, torch.cuda.Stream):
+        return _torch.cuda.current_stream(dev).cuda_stream
+    if isinstance(stream, _torch.cuda.Stream):
         return stream.cuda_stream
     return int(stream)
 
@@ -356,14 +355,13 @@ def _empty(shape, dtype, dev, stream, owned):
     """A new tensor for a launch on ``stream``, in memory of that stream: what
     torch's current stream has freed may still be in use by work queued there,
     which the launch does not wait for."""
-    import torch
     if stream is None:
-        t = torch.empty(shape, dtype=dtype, device=dev)
+        t = _torch.empty(shape, dtype=dtype, device=dev)
     else:
-        if not isinstance(stream, torch.cuda.Stream):
-            stream = torch.cuda.ExternalStream(int(stream), device=dev)
-        with torch.cuda.stream(stream):
-            t = torch.empty(shape, dtype=dtype, device=dev)
+        if not isinstance(stream, _torch.cuda.Stream):
+            stream = _torch.cuda.ExternalStream(int(stream), device=dev)
+        with _torch.cuda.stream(stream):
+            t = _torch.empty(shape, dtype=dtype, device=dev)
     owned.append(t)
     return t
 
@@ -376,17 +374,16 @@ def _launch(call, dev, stream, owned, given):
     the caller's is done with it.  The caller's outputs (``given``) count as
     written in place, so that a backward pass that saved one before fails
     instead of reading what is there now."""
-    import torch
-    with torch.cuda.device(dev):
+    with _torch.cuda.device(dev):
         raw = _stream_handle(stream, dev)
         _check(call(ctypes.c_void_p(raw)))
         if owned and stream is not None:
-            current = torch.cuda.current_stream(dev)
+            current = _torch.cuda.current_stream(dev)
             if raw != current.cuda_stream:
                 for t in owned:
                     t.record_stream(current)
     if given:
-        torch.autograd.graph.increment_version(given)
+        _torch.autograd.graph.increment_version(given)
 
 
 def _handles(lm, boost):
@@ -555,13 +552,13 @@ def ctcbeam_decode_noalloc(logprobs, lengths, K: int, alpha: float = 0.0, beta: 
 def ctcbeam_query_status(workspace, stream=None) -> int:
     """Status bits (ORed over utterances) of the last decode that used
     ``workspace``; synchronises ``stream`` (default: torch's current one)."""
-    import torch
+    lib = _load()
     dev = workspace.device
     bits = ctypes.c_uint32(0)
-    with torch.cuda.device(dev):
+    with _torch.cuda.device(dev):
         raw = _stream_handle(stream, dev)
-        _check(_load().ctcbeam_query_status(ctypes.c_void_p(workspace.data_ptr()),
-                                            ctypes.c_void_p(raw), ctypes.byref(bits)))
+        _check(lib.ctcbeam_query_status(ctypes.c_void_p(workspace.data_ptr()),
+                                        ctypes.c_void_p(raw), ctypes.byref(bits)))
     return int(bits.value)
 
 

@@ -59,3 +59,16 @@ def test_outputs_in_use_on_the_current_stream_are_not_reused():
         torch.cuda.synchronize()
         assert not reused
         del again
+
+
+def test_the_default_stream_by_its_handle():
+    """Handle 0, with the default stream current and with another one."""
+    for call in calls():
+        want = call(None)
+        torch.cuda.synchronize()
+        for current in (torch.cuda.default_stream(), torch.cuda.Stream()):
+            with torch.cuda.stream(current):
+                got = call(0)
+            torch.cuda.synchronize()
+            outputs = [(a, b) for a, b in zip(got, want) if a is not None and a.dtype != torch.uint8]
+            assert all(torch.equal(a, b) for a, b in outputs)

@@ -393,7 +393,8 @@ int ctcbeam_top_logits(const ctcbeam_rows* logits, int k, float temperature, flo
  * NaN.
  *   top_values, top_ids : device [B, T, k], k in 1..CTCBEAM_MAX_TOP
  *   temperature : as for ctcbeam_top_logits
- *   tail    : device [B, T] or NULL, log-sum at `temperature`
+ *   tail    : device [B, T] or NULL, log-sum at `temperature`; NaN counts as
+ *             -inf, +inf as the largest finite number
  *   weights : device, weight of row (b, t) at b*weight_stride_b +
  *             t*weight_stride_t, or NULL: `weight`.  Only grad is weighted.
  *   loss    : device fp32 [B, T], or NULL

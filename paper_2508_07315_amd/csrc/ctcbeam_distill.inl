@@ -342,7 +342,7 @@ distill_kernel(const DistillParams p, const DistillPlan plan, SpanSums* sums) {
   }
 }
 
-// Rows that a workgroup holds in packed registers.  A bit per
+// Rows that a workgroup holds in packed registers (up to 124, none spilled).  A bit per
 // label in LDS says which are listed; few vectors of a wave hold one, and only
 // those look their gradient up, in a table of four places an entry, each
 // label at the first free one from its own on.  One workgroup fills a compute unit, so reading,

@@ -32,7 +32,9 @@ namespace rows {
 enum Phase { kWhole = 0, kStats = 1, kFinish = 2 };
 
 // (four waves a SIMD for 32 labels a thread: 16.4 us against 21 for the second
-// launch above; more waves, or any bound for fewer labels, spill)
+// launch above, though at 128 registers the second launch and the whole-row form
+// spill 12 to 16 of them for 16-bit rows, 6 for fp32, 28 to 60 bytes a lane.  The forms
+// of fewer labels spill none, and would under a bound: 57 us against 45)
 template <typename T, int N, int F, int PHASE>
 __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(F == 32 ? 4 : 1)))
 process_kernel(const ProcessParams p, const ProcessPlan plan, Part* parts) {

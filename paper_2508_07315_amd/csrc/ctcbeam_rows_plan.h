@@ -31,12 +31,18 @@ inline ProcessPlan plan_process(int B, int T, int W, int H, bool normalize, int*
   ProcessPlan q{1, W, 1, T};
   if (W < kRowOfWave && rows >= 1024) {
     // a wave a row, also where an utterance has fewer frames than a workgroup
-    // waves: 4096 requests, T = 1, bf16, us by waves / by workgroups: 33 labels
-    // 6.0 / 9.1, 1025 8.6 / 13.4, 2000 12.8 / 16.0
+    // waves, whose others then leave at once: 4096 requests, T = 1, bf16, us by waves
+    // / by workgroups: 33 labels 6.0 / 9.1, 1025 8.6 / 13.4, 2000 12.8 / 16.0, 2303
+    // 14.6 / 13.1; fp32 33 labels 6.1 / 8.5, 1025 9.2 / 10.5, 2303 15.8 / 13.3.
+    // 512 requests of 1025: 3.8 / 4.3, fp32 4.0 / 3.9
     *n = 64;
     *f = W < 64 * 20 ? 16 : 32;
     q.frames = 4;
   } else if (W < kRowOfGroup && (normalize || rows >= 512)) {
+    // by a workgroup a row / by spans, fp32 (bf16 within 0.5 us): 256 rows of 9200
+    // normalised 7.9 / 11.5, 1024 rows 15.1 / 26.9; not normalised, of one launch
+    // either way, 1 row 4.3 / 2.8, 256 rows 7.0 / 6.8, 1024 rows 14.3 / 16.1, and of
+    // 2400 labels 3.4 / 3.3 (256 rows), 3.9 / 5.1 (512 rows)
     *n = 256;
     *f = W < 256 * 12 ? 8 : W < 256 * 20 ? 16 : 32;
   } else {
@@ -66,9 +72,16 @@ struct TopPlan {
 
 // A wave for each of many short rows; 256 threads for short rows; for longer
 // ones the fewest threads that hold the row where there are rows for every
-// compute unit, else 1024.  bf16, k = 64, us by the fewest / by 1024 threads: 1 row of
-// 32768 labels 13.6 / 7.6; 512 rows 18.7 / 18.2, 1024 rows 25.8 / 34.1, 2048 rows
-// 41 / 63; 2048 rows of 65536 72 / 100.
+// compute unit, else 1024.
+// By a wave / by 256 threads, k = 32, us, bf16: 33 labels, 512 rows 3.8 / 4.9, 1024 rows
+// 3.9 / 5.4, 25600 rows 16 / 56; 1025 labels 5.0 / 5.9, 5.1 / 6.6, 26 / 78; 2303 labels
+// 5.8 / 5.8, 6.0 / 6.6, 39 / 81; fp32, 2303 labels 6.0 / 5.9, 6.4 / 6.9, 53 / 70.
+// By the fewest / by 1024 threads, us, bf16: 1 row of 32768 labels, k = 64, 13.6 / 7.6; 512
+// rows 18.7 / 18.2, 1024 rows 25.8 / 34.1, 2048 rows 41 / 63; 2048 rows of 65536 72 / 100.
+// 512 rows of 34700: k = 16 16.5 / 16.4, k = 128 25.0 / 24.4; 1024 rows 22 / 29, 33 / 45.
+// fp32 crosses later: 17300 labels, k = 16, 512 rows 13.5 / 11.4, 1024 rows 18.5 / 17.7, 2048
+// rows 31 / 32 (k = 128 20.6 / 16.5, 27.6 / 26.9, 47 / 49); 34700 labels 18.2 / 21.4, 33 / 43,
+// 55 / 80.
 inline TopPlan plan_top(int type, int B, int T, int W, int k) {
   const int64_t rows = static_cast<int64_t>(B) * T;
   const int vec = type == kTypeF32 ? 4 : 8;
@@ -100,16 +113,28 @@ struct DistillPlan {
 //   32768        9.9 / 7.9  12.3 / 12.0 13.3 / 14.7 14.6 / 17.5
 //   65536       15.7 / 7.7  19.3 / 16.4 20.2 / 21.1 23.3 / 27.2
 //   131072      27.0 / 7.7  33.3 / 26.7 36.3 / 39.3 39.7 / 47.6
+// k = 128 lies on the same sides (65536 labels, 128 rows 20.3 / 18.4, 160 rows 20.9 /
+// 20.1, 192 rows 22.0 / 22.2).  fp32 rows of as many labels are twice the bytes, and
+// spans pay for fewer of them, k = 16:
+//   24600        7.7 / 8.3  11.1 / 15.0 12.6 / 17.6 13.9 / 18.9
+//   32768        8.3 / 8.1  12.0 / 16.0 13.7 / 20.0 16.4 / 21.5
+//   65536       12.7 / 8.0  18.7 / 21.5 25.8 / 36.5 30.8 / 51.5
 constexpr int64_t kFewRows = 160;
 constexpr int kLongRow = 24576;
 // Rows from which on smaller workgroups, several of a compute unit, take rows of
 // fewer than 512 * 17 vectors, us by them / by 1024 threads: 18400 labels, 512 rows
 // 17.7 / 18.9, 2048 rows 40 / 64; 65536 labels, 512 rows 38 / 43,
-// 2048 rows 131 / 171.
+// 2048 rows 131 / 171.  fp32, k = 16: 9300 labels, 256 rows 10.1 / 8.6, 512 rows 13.1 /
+// 15.4, 2048 rows 40 / 58; 34700 labels 17.9 / 17.0, 32 / 39, 119 / 126; k = 128
+// 20.3 / 18.7, 35 / 42, 130 / 143.
 constexpr int64_t kManyRows = 512;
 
 inline DistillPlan plan_distill(int type, int B, int T, int W) {
   const int64_t rows = static_cast<int64_t>(B) * T;
+  // by a wave / by 256 threads, k = 16, us, bf16: 33 labels, 512 rows 4.2 / 4.8, 1024
+  // rows 4.3 / 5.4; 1025 labels 4.8 / 5.8, 4.9 / 6.9, 25600 rows 31 / 77; 2303 labels 6.3 /
+  // 5.3, 6.6 / 6.5, 53 / 77; fp32, 1025 labels 5.0 / 5.1, 5.3 / 6.0, 47 / 71; 2303
+  // 6.9 / 5.5, 8.5 / 7.8, 97 / 90
   if (W < 64 * 36 && rows >= 1024) return {64, W < 64 * 20 ? 16 : 32, 1, W};
   if (W < 256 * 36) return {256, W < 256 * 12 ? 8 : W < 256 * 20 ? 16 : 32, 1, W};
   const int vec = type == kTypeF32 ? 4 : 8;

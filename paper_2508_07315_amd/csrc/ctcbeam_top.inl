@@ -9,14 +9,16 @@
 // room for lie above the bound (rows of equal values), the k-th label is found
 // exactly, bit by bit.
 //
-// What bounds it: for long rows reading them (2048 rows of 65537 bf16 labels,
-// k = 64: 268 MB in 83 us, 3.2 TB/s, where a library maximum over the same rows
-// reads 3.75 TB/s), since a vector of which no wave holds a label above the
-// bound costs a conversion, a comparison and an exponential a label.  For short
-// rows what comes after the reading: 19200 rows of 1025, k = 16, take 20 us,
-// twice the time to read them, for the bound's 16 steps, the places and the
-// sums.  Loading the taken labels again from memory or from a copy of the row
-// in LDS takes the same time.
+// What bounds it: for long rows the reading and what follows it in the same
+// workgroup (2048 rows of 65537 labels, k = 64: bf16 268 MB in 83 us, 3.2 TB/s, fp32
+// 537 MB in 148 us, 3.6 TB/s, where a copy moves 4.96 TB/s), as a vector of which
+// no wave holds a label above the bound costs a conversion, a comparison and an
+// exponential a label, and those wait for the bound, so for the whole row.  For
+// shorter rows the chain after the reading: 19200 rows of 1025 bf16 labels, k = 16,
+// take 20 us, 2048 rows of 9300, k = 64, 22 us, twice and three times the time to
+// read them, for the bound's 16 dependent steps, the places (each taken label
+// against all) and the sums.  Loading the taken labels again from memory or from
+// a copy of the row in LDS takes the same time.
 //
 // A wave takes rows of fewer than 2304 labels (lists of up to 32), a workgroup of
 // 256 to 1024 threads longer ones; rows beyond a workgroup are cut into spans
@@ -77,7 +79,9 @@ __device__ __forceinline__ float group_max(float v, int group) {
 }
 
 // (four waves a SIMD for 16 vectors a thread: two workgroups of 512 a compute
-// unit, 87 us against 139 for 2048 rows of 65537)
+// unit, 87 us against 139 for 2048 rows of 65537; at 128 registers the 16-bit forms
+// spill 10 of them at 256 and 512 threads, 24 bytes a lane, and 19 to 36 at 1024, 48
+// bytes; the fp32 forms none)
 template <typename T, int N, int VECS, bool PART>
 __global__ void __launch_bounds__(N > kThreads ? N : kThreads) __attribute__((amdgpu_waves_per_eu(VECS == 16 ? 4 : 1)))
 top_kernel(const TopParams p, const TopPlan plan, void* ws) {

@@ -288,8 +288,9 @@ int ctcbeam_query_status(const void* workspace, hipStream_t stream, uint32_t* bi
  * Operators on rows of scores, one row per frame: what makes the decoders'
  * input of a model's logits, and what trains the model on a teacher's frames.
  * The call only enqueues kernels on `stream` (no host synchronisation, no
- * allocation); concurrent calls need distinct workspaces.  Outputs may not
- * overlap inputs or each other, except where a call says so (returns 1).
+ * allocation); concurrent calls need distinct workspaces.  Outputs and the
+ * workspace may not overlap inputs or each other, except where a call says so
+ * (returns 1).
  */
 #define CTCBEAM_TYPE_F32 0
 #define CTCBEAM_TYPE_F16 1

@@ -673,8 +673,9 @@ def ctcbeam_process_logits(logits, lengths=None, history=None, history_lengths=N
     [B, T, ceil(W/32)], bit c%32 of word c/32 set where label c is allowed.
     ``normalize=False`` leaves out the log-softmax.  Frames behind an
     utterance's length are left as they were in ``out``, which may be the
-    logits themselves where those are contiguous float32.  No gradient flows
-    through this call.  Returns (float32 [B, T, W], workspace or None)."""
+    logits themselves where those are contiguous float32 (detached, if torch
+    records a gradient for them).  No gradient flows through this call.
+    Returns (float32 [B, T, W], workspace or None)."""
     lib = _load()
     rows, B, T, W, dev = _rows_of(logits, lengths, "logits")
     owned, given = [], []

@@ -217,3 +217,14 @@ def test_small_temperatures():
         assert torch.equal(ids.cpu(), R.top(x, 2)[1]) and not torch.isnan(tail).any()
         loss, grad = P.distill(x, v, ids, tail, temperature=4.3e-39)
         assert not torch.isnan(loss).any() and not torch.isnan(grad).any()
+
+
+def test_tails_that_are_no_number():
+    """NaN counts as -inf, +inf as the largest number."""
+    for B, T, W in ((2, 3, 40), (300, 4, 33), (2, 3, 2500), (2, 3, 9300), (1, 2, 150000)):
+        x = scores(B, T, W, "fp32", W)
+        v, ids, tail = P.top_logits(x, 4)
+        for odd, plain in ((math.nan, -INF), (INF, R.LARGEST)):
+            a, b = tail.clone(), tail.clone()
+            a[0, 1], b[0, 1] = odd, plain
+            assert all(torch.equal(p, q) for p, q in zip(P.distill(x * 0.5, v, ids, a), P.distill(x * 0.5, v, ids, b)))
